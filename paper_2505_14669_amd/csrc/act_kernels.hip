@@ -1,0 +1,106 @@
+// Backward pass of the product's epilogue: dz = dy * multiplier * a'(z), dmul = dy * a(z), and the bias's gradient, the column sums of dz.
+// Bound by memory: 2 bytes each of dy, z, the multiplier, dz and dmul per element, one pass.  A block is four waves over 512 columns (a lane
+// holds eight of them: 16-byte accesses, a kilobyte per wave and row) and a stretch of rows, so the column sums stay in registers until the stretch ends.
+#include "block_common.h"
+#include "block_launchers.h"
+
+namespace quartet {
+
+namespace {
+
+// the first `left` of eight bf16 values (8 and more: all)
+__device__ __forceinline__ uint4 load_bf16x8(const uint16_t* p, int left) {
+    if (left >= 8) return *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_bf16x8(uint16_t* p, int left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<uint4*>(p) = pack8(v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) p[i] = bf16_of(v[i]);
+}
+
+__global__ void __launch_bounds__(256)
+act_bwd_kernel(ActBwdArgs a, uint32_t col_blocks, FastDiv by_col_blocks, uint32_t rows_per_block) {
+    __shared__ float4 join[4][128];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t stretch = fast_div(blockIdx.x, by_col_blocks), col = ((blockIdx.x - stretch * col_blocks) * 64u + lane) * 8u;
+    const int left = (int)a.n - (int)col;
+    const uint32_t row0 = stretch * rows_per_block, row1 = a.m - row0 < rows_per_block ? a.m : row0 + rows_per_block;
+    float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (left > 0) {
+        for (uint32_t row = row0 + wave; row < row1; row += 4u) {
+            float dy[8], z[8], mul[8], value[8], slope[8];
+            unpack8(load_bf16x8(a.dy + (size_t)row * a.lddy + col, left), dy);
+            if (a.pre) unpack8(load_bf16x8(a.pre + (size_t)row * a.ldpre + col, left), z);
+            else for (int i = 0; i < 8; ++i) z[i] = 0.0f;
+            if (a.mul) unpack8(load_bf16x8(a.mul + (size_t)row * a.ldmul + col, left), mul);
+            activate_slope(z, value, slope, a.act);
+            float dz[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                value[i] *= dy[i];
+                dz[i] = (a.mul ? dy[i] * mul[i] : dy[i]) * slope[i];
+                sum[i] += dz[i];
+            }
+            if (a.dz) store_bf16x8(a.dz + (size_t)row * a.lddz + col, left, dz);
+            if (a.dmul) store_bf16x8(a.dmul + (size_t)row * a.lddmul + col, left, value);
+        }
+    }
+    if (!a.partial) return;
+    join[wave][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    join[wave][64u + lane] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    __syncthreads();
+    // thread t: half t / 64 % 2 of lane t % 64's eight columns
+    if (threadIdx.x < 128u) {
+        float4 s = join[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            const float4 t = join[w][threadIdx.x];
+            s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+        }
+        const uint32_t pitch = (a.n + 7u) & ~7u;
+        if (col < pitch) *reinterpret_cast<float4*>(a.partial + (size_t)stretch * pitch + col + (threadIdx.x >> 6) * 4u) = s;
+    }
+}
+
+struct ActPlan {
+    uint32_t col_blocks, stretches, rows_per_block;
+};
+// Blocks of 512 columns x a stretch of rows: at least 16 rows (four per wave), and about 2048 blocks in all (eight per compute unit).
+ActPlan act_plan(int64_t m, int64_t n) {
+    const int64_t cb = (n + 511) / 512;
+    int64_t rows = (m * cb + 2047) / 2048;
+    rows = (rows + 3) / 4 * 4;
+    if (rows > m) rows = m;
+    if (rows < 16) rows = 16;
+    return {(uint32_t)cb, (uint32_t)((m + rows - 1) / rows), (uint32_t)rows};
+}
+
+}  // namespace
+
+size_t act_bwd_workspace(int64_t m, int64_t n) {
+    if (m <= 0 || n <= 0) return 0;
+    return (size_t)act_plan(m, n).stretches * (size_t)((n + 7) / 8 * 8) * sizeof(float);
+}
+
+hipError_t launch_act_bwd(const ActBwdArgs& args, float* dbias, float* workspace, hipStream_t st) {
+    if (args.n == 0) return hipSuccess;
+    if (args.m == 0) return dbias ? launch_column_sum(nullptr, 0u, 0u, args.n, dbias, st) : hipSuccess;
+    ActBwdArgs a = args;
+    a.partial = dbias ? workspace : nullptr;
+    const ActPlan p = act_plan(a.m, a.n);
+    hipLaunchKernelGGL(act_bwd_kernel, dim3(p.col_blocks * p.stretches), dim3(256), 0, st, a, p.col_blocks, make_fast_div(p.col_blocks), p.rows_per_block);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !dbias) return e;
+    return launch_column_sum(workspace, p.stretches, (a.n + 7u) & ~7u, a.n, dbias, st);
+}
+
+}  // namespace quartet

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "api_common.h"
 #include "device_common.h"
 #include "launchers.h"
 
@@ -11,12 +12,9 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-int hip_fail(hipError_t e) {
-    g_last_hip_error = (int)e;
-    return QUARTET_EHIP;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using quartet::aligned16;
+using quartet::hip_fail;
+using quartet::ProfileScope;
 
 // Philox4x32-10 on the host (Salmon et al., SC'11), used only to derive the sign word.
 void philox_host(const uint32_t ctr[4], const uint32_t key[2], uint32_t out[4]) {
@@ -71,21 +69,6 @@ struct ProfileState {
     int* kind = nullptr;
 };
 ProfileState g_prof;
-
-struct ProfileScope {
-    int slot = -1;
-    hipStream_t st;
-    ProfileScope(int kind, hipStream_t s) : st(s) {
-        if (g_prof.enabled && ((g_prof.kinds >> kind) & 1u) && g_prof.count < g_prof.capacity) {
-            slot = g_prof.count++;
-            g_prof.kind[slot] = kind;
-            (void)hipEventRecord(g_prof.start[slot], st);
-        }
-    }
-    ~ProfileScope() {
-        if (slot >= 0) (void)hipEventRecord(g_prof.stop[slot], st);
-    }
-};
 
 void profile_free() {
     for (int i = 0; i < g_prof.capacity; ++i) {
@@ -160,7 +143,38 @@ int static_scratch(void** out) {
 
 }  // namespace
 
+int quartet::hip_fail(hipError_t e) {
+    g_last_hip_error = (int)e;
+    return QUARTET_EHIP;
+}
+
+quartet::ProfileScope::ProfileScope(int kind, hipStream_t s) : st(s) {
+    if (g_prof.enabled && ((g_prof.kinds >> kind) & 1u) && g_prof.count < g_prof.capacity) {
+        slot = g_prof.count++;
+        g_prof.kind[slot] = kind;
+        (void)hipEventRecord(g_prof.start[slot], st);
+    }
+}
+quartet::ProfileScope::~ProfileScope() {
+    if (slot >= 0) (void)hipEventRecord(g_prof.stop[slot], st);
+}
+
+int quartet::check_gemm_args(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
+                             const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, const void* d, int d_dtype,
+                             int64_t ldd) {
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !d) return QUARTET_EINVAL;
+    if (!aligned16(a_codes) || !aligned16(b_codes) || !aligned16(d)) return QUARTET_EINVAL;
+    if (m < 0 || n < 0 || k < 0 || (k % 32) != 0 || ldd < n) return QUARTET_EINVAL;
+    if (ldd > ((int64_t)1 << 21)) return QUARTET_ENOTSUP;
+    if (d_dtype != QUARTET_DTYPE_F32 && d_dtype != QUARTET_DTYPE_BF16) return QUARTET_EINVAL;
+    if (m >= ((int64_t)1 << 31) || n >= ((int64_t)1 << 31) || k > ((int64_t)1 << 23)) return QUARTET_ENOTSUP;
+    if (((m + 127) / 128) * ((n + 127) / 128) >= ((int64_t)1 << 31)) return QUARTET_ENOTSUP;
+    if ((reinterpret_cast<uintptr_t>(a_scales) | reinterpret_cast<uintptr_t>(b_scales)) & 3u) return QUARTET_EINVAL;
+    return QUARTET_OK;
+}
+
 using quartet::SrParams;
+using quartet::check_gemm_args;
 
 extern "C" {
 
@@ -399,20 +413,6 @@ int quartet_requant_transpose_sr_block(const uint8_t* src_codes, const uint8_t* 
     hipError_t e = quartet::launch_requant_transpose(mode, src_codes, src_scales, rows, k, p, codes, scales,
                                                      (hipStream_t)stream);
     return e == hipSuccess ? QUARTET_OK : hip_fail(e);
-}
-
-static int check_gemm_args(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
-                           const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, const void* d, int d_dtype,
-                           int64_t ldd) {
-    if (!a_codes || !a_scales || !b_codes || !b_scales || !d) return QUARTET_EINVAL;
-    if (!aligned16(a_codes) || !aligned16(b_codes) || !aligned16(d)) return QUARTET_EINVAL;
-    if (m < 0 || n < 0 || k < 0 || (k % 32) != 0 || ldd < n) return QUARTET_EINVAL;
-    if (ldd > ((int64_t)1 << 21)) return QUARTET_ENOTSUP;
-    if (d_dtype != QUARTET_DTYPE_F32 && d_dtype != QUARTET_DTYPE_BF16) return QUARTET_EINVAL;
-    if (m >= ((int64_t)1 << 31) || n >= ((int64_t)1 << 31) || k > ((int64_t)1 << 23)) return QUARTET_ENOTSUP;
-    if (((m + 127) / 128) * ((n + 127) / 128) >= ((int64_t)1 << 31)) return QUARTET_ENOTSUP;
-    if ((reinterpret_cast<uintptr_t>(a_scales) | reinterpret_cast<uintptr_t>(b_scales)) & 3u) return QUARTET_EINVAL;
-    return QUARTET_OK;
 }
 
 int quartet_mxfp4_gemm(const uint8_t* a_codes, const uint8_t* a_scales,

@@ -26,6 +26,7 @@
 // (layer steps, us): 16384 x 4096 x 11008 1434 -> 1378, 16384 x 4096 x 4096 620 -> 601, 2336 x 1376 x 3168 78.7 -> 71.5, 4096 x 2048 x 2048
 // 91.2 -> 85.1, forward 1003 x 2048 x 5632 25.6 -> 23.9.  (16 x 16 x 128 on the old stages: 0-4 % slower.)
 #include "gemm_common.h"
+#include "block_launchers.h"
 #include "launchers.h"
 #include "pair_level.h"
 
@@ -974,6 +975,13 @@ hipError_t launch_gemm_grad_pair(const GemmArgs& g0, const GemmArgs& g1, int d_b
     else QUARTET_PAIR(launch_stream_batch_t, );
 #undef QUARTET_PAIR
     return hipGetLastError();
+}
+
+hipError_t launch_gemm_act(const GemmArgs& g, const GemmActArgs& act, int d_bf16, hipStream_t st) {
+    if (g.m == 0 || g.n == 0) return hipSuccess;
+    int shape = 0;
+    best_split_shape(1, &g.m, &g.n, &g.k, stream_blocks(), &shape);
+    return launch_gemm_act_split(g, act, d_bf16, shape, st);
 }
 
 }  // namespace quartet

@@ -7,7 +7,7 @@
 // through an LDS ring of its own (two quads of LDS-direct loads, whole 128-byte lines; no barrier in the loop), and the partial
 // sums meet in LDS.  The order of a result's sum depends on k and the number of waves alone, not on the tile shape, and the number of
 // waves on k (of a pair on the larger k), so fused and plain products give the same bits.
-#include "gemm_common.h"
+#include "gemm_act.h"
 #include "launchers.h"
 
 namespace quartet {
@@ -102,9 +102,12 @@ __device__ __forceinline__ void finish_row_chunk(float (&vv)[TN][4], void* d, ui
     }
 }
 
-template <int TM, int TN, int NW, bool OUT_BF16, bool FUSED>
+// E: none, or GemmActArgs: the epilogue of quartet_mxfp4_gemm_act (one product).  (As a device function that two kernels share, the plain kernels'
+// code came out different.)
+template <int TM, int TN, int NW, bool OUT_BF16, bool FUSED, typename... E>
 __global__ void __launch_bounds__(64 * NW)
-gemm_mxfp4_split_kernel(SplitBatch batch, uint32_t nb) {
+gemm_mxfp4_split_kernel(SplitBatch batch, uint32_t nb, E... epilogue) {
+    constexpr bool ACT = sizeof...(E) == 1;
     constexpr uint32_t BM = 32 * TM, BN = 32 * TN, T = TM + TN;
     // a ring slot: T row blocks of 32 rows x 128 bytes (16-byte chunk c of row r at position c ^ (r / 2) % 8: the 16 lanes of a
     // fragment read fall on different banks), then their T scale tiles of 256 bytes
@@ -159,6 +162,21 @@ gemm_mxfp4_split_kernel(SplitBatch batch, uint32_t nb) {
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    // the epilogue's operands are on their way before the product's: nothing waits for them at the end
+    constexpr uint32_t TURNS = ACT ? BM / (8u * NW) : 1u;
+    ActChunk extra[TURNS][TN];
+    float bias[TN][4];
+    if constexpr (ACT) {
+        const GemmActArgs& act = (epilogue, ...);
+        const bool act_whole = act_wide(act, q.ldd);
+        const uint32_t col0 = n0 + 4u * ((tid & 7u) ^ ((tid & 4u) ? 3u : 0u));
+#pragma unroll
+        for (uint32_t t = 0; t < TURNS; ++t)
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) load_act_chunk(extra[t][j], act, m0 + (tid >> 3) + t * 8u * NW, col0 + j * 32u, m, n, act_whole);
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) load_bias(bias[j], act, col0 + j * 32u, n);
+    }
     issue(wave, 0u);
     if (D == 2u) issue(wave + NW, 1u);
     uint32_t slot = 0u;
@@ -226,7 +244,22 @@ gemm_mxfp4_split_kernel(SplitBatch batch, uint32_t nb) {
                 for (uint32_t e = 0; e < 4; ++e) vv[j][e] = u2f(f2u(vv[j][e]) & (uint32_t)((bits << (31 - (int)e)) >> 31));
             }
         }
-        finish_row_chunk<TN, OUT_BF16, FUSED>(vv, q.d, q.ldd, q.alpha, grow, n0, m, n, c, nb);
+        if constexpr (ACT) {
+            const GemmActArgs& act = (epilogue, ...);
+            const bool act_whole = act_wide(act, q.ldd);
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) {
+                const uint32_t col = n0 + j * 32u + 4u * c;
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) vv[j][e] = vv[j][e] * q.alpha + bias[j][e];
+                if (act.pre) store_act_chunk<true>(act.pre, act.ldpre, grow, col, m, n, act_whole, vv[j]);
+                activate(vv[j], act.act);
+                combine_act_chunk(vv[j], extra[(row - (tid >> 3)) / (8u * NW)][j], act);
+                store_act_chunk<OUT_BF16>(q.d, q.ldd, grow, col, m, n, act_whole, vv[j]);
+            }
+        } else {
+            finish_row_chunk<TN, OUT_BF16, FUSED>(vv, q.d, q.ldd, q.alpha, grow, n0, m, n, c, nb);
+        }
     }
 }
 
@@ -307,6 +340,29 @@ hipError_t launch_gemm_split(const GemmArgs& g0, const GemmArgs* g1, int d_bf16,
     default: launch_split<2, 2, NW>(g0, g1, d_bf16, fused, nb, st); break;                              \
     }
     if (split_waves(k) == 4) QUARTET_SPLIT(4)
+    else QUARTET_SPLIT(2)
+#undef QUARTET_SPLIT
+    return hipGetLastError();
+}
+
+template <int TM, int TN, int NW>
+static void launch_split_act(const GemmArgs& g, const GemmActArgs& act, int d_bf16, hipStream_t st) {
+    SplitBatch batch;
+    batch.p[0] = split_problem(g, 32 * TM, 32 * TN);
+    batch.p[1] = SplitProblem{};
+    const dim3 grid(batch.p[0].total_tiles), block(64 * NW);
+    if (d_bf16) hipLaunchKernelGGL((gemm_mxfp4_split_kernel<TM, TN, NW, true, false, GemmActArgs>), grid, block, 0, st, batch, 1u, act);
+    else hipLaunchKernelGGL((gemm_mxfp4_split_kernel<TM, TN, NW, false, false, GemmActArgs>), grid, block, 0, st, batch, 1u, act);
+}
+
+hipError_t launch_gemm_act_split(const GemmArgs& g, const GemmActArgs& act, int d_bf16, int shape, hipStream_t st) {
+#define QUARTET_SPLIT(NW)                                                                               \
+    switch (shape) {                                                                                    \
+    case 11: launch_split_act<1, 1, NW>(g, act, d_bf16, st); break;                                     \
+    case 12: launch_split_act<1, 2, NW>(g, act, d_bf16, st); break;                                     \
+    default: launch_split_act<2, 2, NW>(g, act, d_bf16, st); break;                                     \
+    }
+    if (split_waves(g.k) == 4) QUARTET_SPLIT(4)
     else QUARTET_SPLIT(2)
 #undef QUARTET_SPLIT
     return hipGetLastError();

@@ -23,7 +23,7 @@
 #include <torch/csrc/autograd/VariableTypeUtils.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
-#include "../../include/quartet.h"
+#include "../../include/quartet_block.h"
 
 namespace {
 
@@ -333,6 +333,11 @@ PyMethodDef methods[] = {
     ENTRY_POINT(quartet_quant_bwd_sr),
     ENTRY_POINT(quartet_mxfp4_gemm),
     ENTRY_POINT(quartet_mxfp4_gemm_grad),
+    ENTRY_POINT(quartet_mxfp4_gemm_act),
+    ENTRY_POINT(quartet_act_bwd),
+    ENTRY_POINT(quartet_rmsnorm_fwd),
+    ENTRY_POINT(quartet_rmsnorm_bwd),
+    ENTRY_POINT(quartet_grad_clip),
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_linear)), METH_FASTCALL, nullptr},
     {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_forward)), METH_FASTCALL, nullptr},
     {"backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_backward)), METH_FASTCALL, nullptr},

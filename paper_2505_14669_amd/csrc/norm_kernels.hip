@@ -1,0 +1,444 @@
+// Root-mean-square norm of the residual stream, into bf16 or straight into a linear layer's MX operand, and its backward pass.
+#include "block_common.h"
+#include "block_launchers.h"
+
+namespace quartet {
+
+namespace {
+
+constexpr int kFmtNone = 0, kFmtMx4 = 1, kFmtMx8 = 2;
+typedef short v2s_t __attribute__((ext_vector_type(2)));
+
+// four values, |v| <= 448, -> four E4M3 bytes, round to nearest even
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+    v2s_t w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, 1.0f, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, 1.0f, true);
+    return (uint32_t)(uint16_t)w[0] | ((uint32_t)(uint16_t)w[1] << 16);
+}
+// eight values -> eight E2M1 codes of v / scale, round to nearest even, saturating
+__device__ __forceinline__ uint32_t e2m1x8(const float* v, float scale) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+    return c;
+}
+
+// One row of a matrix as a buffer resource over its whole chunks of eight values: a load past them gives zeros, a store past them is dropped, so
+// the lanes beyond the row need no branches.  The n % 8 values behind the last whole chunk go one by one.
+struct Row {
+    __amdgpu_buffer_rsrc_t res;
+    uint8_t* tail;            // the values behind the whole chunks
+    uint32_t bytes;           // per value
+};
+__device__ __forceinline__ Row row_of(const void* p, bool f32, size_t at, uint32_t n) {     // n = 0: no row
+    const uint32_t bytes = f32 ? 4u : 2u;
+    uint8_t* base = static_cast<uint8_t*>(const_cast<void*>(p)) + at * bytes;
+    return {__builtin_amdgcn_make_buffer_rsrc(base, 0, (n & ~7u) * bytes, 0x00020000), base + (size_t)(n & ~7u) * bytes, bytes};
+}
+__device__ __forceinline__ uint4 u4(v4u_t v) { return make_uint4(v.x, v.y, v.z, v.w); }
+
+// eight consecutive values as they lie in memory
+struct Raw8 {
+    uint4 lo, hi;      // bf16: lo
+};
+__device__ __forceinline__ void load8(Raw8& r, const Row& row, bool f32, uint32_t col) {
+    if (f32) {
+        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u), 0, 0));
+        r.hi = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u + 16u), 0, 0));
+    } else {
+        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 2u), 0, 0));
+    }
+}
+// the lane whose columns are the row's last, incomplete chunk: `left` = 1 .. 7 values (other lanes: 0)
+__device__ __forceinline__ void load_tail(Raw8& r, const Row& row, bool f32, uint32_t left) {
+    if (left == 0u) return;
+    uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+    for (uint32_t i = 0; i < 7; ++i)
+        if (i < left) {
+            if (f32) w[i] = reinterpret_cast<const uint32_t*>(row.tail)[i];
+            else w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row.tail)[i] << (16u * (i & 1u));
+        }
+    r.lo = make_uint4(w[0], w[1], w[2], w[3]);
+    r.hi = make_uint4(w[4], w[5], w[6], w[7]);
+}
+__device__ __forceinline__ void values8(const Raw8& r, bool f32, float* v) {
+    if (f32) {
+        v[0] = u2f(r.lo.x); v[1] = u2f(r.lo.y); v[2] = u2f(r.lo.z); v[3] = u2f(r.lo.w);
+        v[4] = u2f(r.hi.x); v[5] = u2f(r.hi.y); v[6] = u2f(r.hi.z); v[7] = u2f(r.hi.w);
+    } else {
+        unpack8(r.lo, v);
+    }
+}
+__device__ __forceinline__ void store8(const Row& row, bool f32, uint32_t col, uint32_t tail, const float* v) {
+    if (f32) {
+        const v4u_t lo = {f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])}, hi = {f2u(v[4]), f2u(v[5]), f2u(v[6]), f2u(v[7])};
+        __builtin_amdgcn_raw_buffer_store_b128(lo, row.res, (int)(col * 4u), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(hi, row.res, (int)(col * 4u + 16u), 0, 0);
+    } else {
+        const uint4 q = pack8(v);
+        const v4u_t d = {q.x, q.y, q.z, q.w};
+        __builtin_amdgcn_raw_buffer_store_b128(d, row.res, (int)(col * 2u), 0, 0);
+    }
+    if (tail == 0u) return;
+#pragma unroll
+    for (uint32_t i = 0; i < 7; ++i)
+        if (i < tail) {
+            if (f32) reinterpret_cast<float*>(row.tail)[i] = v[i];
+            else reinterpret_cast<uint16_t*>(row.tail)[i] = bf16_of(v[i]);
+        }
+}
+// how many values the lane with columns col .. col + 7 has of the row's incomplete chunk
+__device__ __forceinline__ uint32_t tail_of(uint32_t col, uint32_t n) { return col == (n & ~7u) ? n & 7u : 0u; }
+
+// Eight columns of one row in each lane; the WPR waves of a row meet in LDS.
+// sum of `part` over the row's lanes, the same bits in all of them
+template <int WPR>
+__device__ __forceinline__ float row_sum(float part, float* meet, uint32_t slot, uint32_t sub, uint32_t lane) {
+    float s = wave_sum(part);
+    if (WPR == 1) return s;
+    if (lane == 0) meet[slot * WPR + sub] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) s += meet[slot * WPR + w];
+    return s;
+}
+
+// A row belongs to WPR waves; lane l of wave `sub` of a row holds the columns 8 ((j WPR + sub) 64 + l) .. + 7 of chunk j < CH.
+template <int WPR, int CH, int FMT>
+__global__ void __launch_bounds__(WPR < 4 ? 256 : 64 * WPR)
+rmsnorm_fwd_kernel(NormFwdArgs a) {
+    constexpr uint32_t THREADS = WPR < 4 ? 256 : 64 * WPR, RPB = THREADS / 64 / WPR;
+    __shared__ float meet[THREADS / 64];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t slot = wave / WPR, sub = wave % WPR, row = blockIdx.x * RPB + slot;
+    const bool in = row < a.rows;
+    const uint32_t n = a.n;
+    const uint32_t n_in = in ? n : 0u;
+    const Row x_row = row_of(a.x, a.x_f32, (size_t)row * a.ldx, n_in), w_row = row_of(a.weight, a.w_f32, 0, n);
+    const Row r_row = row_of(a.residual, a.h_f32, (size_t)row * a.ldres, a.residual ? n_in : 0u);
+    const Row h_row = row_of(a.h, a.h_f32, (size_t)row * a.ldh, a.h ? n_in : 0u), y_row = row_of(a.y, false, (size_t)row * a.ldy, a.y ? n_in : 0u);
+    Raw8 rx[CH], rr[CH], rw[CH];
+    uint32_t col[CH], tail[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        col[j] = (((uint32_t)j * WPR + sub) * 64u + lane) * 8u;
+        tail[j] = in ? tail_of(col[j], n) : 0u;
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) load8(rx[j], x_row, a.x_f32, col[j]);
+    if (a.residual) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) load8(rr[j], r_row, a.h_f32, col[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) load8(rw[j], w_row, a.w_f32, col[j]);
+    if ((n & 7u) != 0u) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            load_tail(rx[j], x_row, a.x_f32, tail[j]);
+            if (a.residual) load_tail(rr[j], r_row, a.h_f32, tail[j]);
+            load_tail(rw[j], w_row, a.w_f32, tail[j]);
+        }
+    }
+    float v[CH][8];
+    float part = 0.0f;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        values8(rx[j], a.x_f32, v[j]);
+        if (a.residual) {
+            float r[8];
+            values8(rr[j], a.h_f32, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] += r[i];
+            if (!a.h_f32) {                   // the norm reads what the stream holds
+                const uint4 q = pack8(v[j]);
+                unpack8(q, v[j]);
+            }
+            if (a.h) store8(h_row, a.h_f32, col[j], tail[j], v[j]);
+        }
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = v[j][i] * v[j][i];
+        part += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    }
+    const float ss = row_sum<WPR>(part, meet, slot, sub, lane);
+    const float rstd = 1.0f / __builtin_sqrtf(ss / (float)n + a.eps);
+    if (a.rstd && in && sub == 0u && lane == 0u) a.rstd[row] = rstd;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        float w[8];
+        values8(rw[j], a.w_f32, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * rstd * w[i];
+        if (a.y) store8(y_row, false, col[j], tail[j], v[j]);
+        if (FMT == kFmtNone) continue;
+        // a group is four consecutive lanes; n is a multiple of 32, so it exists as a whole or not at all
+        const bool there = in && col[j] < n;
+        const uint32_t g = col[j] >> 5, kqs = (n + 255u) >> 8;
+        if (FMT == kFmtMx8) {
+            float mx = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx = __builtin_fmaxf(mx, __builtin_fabsf(v[j][i]));
+            mx = __builtin_fmaxf(mx, lane_xor<1>(mx));
+            mx = __builtin_fmaxf(mx, lane_xor<2>(mx));
+            const uint32_t E = (f2u(mx) >> 23) & 0xFFu, b = E >= 8u ? E - 8u : 0u;
+            const float mult = u2f((254u - b) << 23);
+            float q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = __builtin_amdgcn_fmed3f(v[j][i] * mult, -448.0f, 448.0f);
+            if (there) {
+                *reinterpret_cast<uint2*>(a.codes + (size_t)row * n + col[j]) = make_uint2(e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7]));
+                if ((lane & 3u) == 0u) a.scales[scale_tile_offset(row, g, kqs)] = (uint8_t)b;
+            }
+        } else {
+            // 32-point transform: strides 1, 2, 4 in the lane, 8 and 16 between lanes (own * t + partner: a + b below, a - b above)
+#pragma unroll
+            for (int h = 1; h < 8; h <<= 1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((i & h) == 0) {
+                        const float p = v[j][i], q = v[j][i + h];
+                        v[j][i] = p + q;
+                        v[j][i + h] = p - q;
+                    }
+            const float t8 = (lane & 1u) ? -1.0f : 1.0f, t16 = (lane & 2u) ? -1.0f : 1.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = __builtin_fmaf(v[j][i], t8, lane_xor<1>(v[j][i]));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = __builtin_fmaf(v[j][i], t16, lane_xor<2>(v[j][i]));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] *= kInvSqrt32;
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = v[j][i] * v[j][i];
+            float sq = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));      // the pairwise tree of quartet_quant_fwd
+            sq += lane_xor<1>(sq);
+            sq += lane_xor<2>(sq);
+            const uint32_t E = (f2u(sq) >> 23) & 0xFFu;
+            const int e = E == 0u ? 0 : ((int)E - 133) >> 1;
+            const uint32_t b = (uint32_t)(e + 127);
+            const float scale = u2f(b << 23), thr = u2f(0x40C00000u + ((uint32_t)e << 23));
+            uint32_t m = 0u;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) m = (m << 1) | (__builtin_fabsf(v[j][i]) <= thr ? 1u : 0u);
+            m <<= 8u * (lane & 3u);
+            m |= f2u(lane_xor<1>(u2f(m)));
+            m |= f2u(lane_xor<2>(u2f(m)));
+            if (there) {
+                *reinterpret_cast<uint32_t*>(a.codes + (size_t)row * (n >> 1) + (col[j] >> 1)) = e2m1x8(v[j], scale);
+                if ((lane & 3u) == 0u) {
+                    a.scales[scale_tile_offset(row, g, kqs)] = (uint8_t)b;
+                    if (a.mask) a.mask[(size_t)row * (n >> 5) + g] = m;
+                }
+            }
+        }
+    }
+}
+
+// Backward: a block goes through the rows blockIdx.x RPB + slot, + gridDim.x RPB, ...; the weight and its gradient's partial sums stay in
+// registers, the latter meet in LDS and go to the workspace, one row of n floats per block.
+template <int WPR, int CH>
+__global__ void __launch_bounds__(WPR < 4 ? 256 : 64 * WPR)
+rmsnorm_bwd_kernel(NormBwdArgs a) {
+    constexpr uint32_t THREADS = WPR < 4 ? 256 : 64 * WPR, RPB = THREADS / 64 / WPR;
+    __shared__ float meet[2][THREADS / 64];
+    __shared__ float4 join[RPB > 1 ? THREADS * 2 : 1];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t slot = wave / WPR, sub = wave % WPR, n = a.n;
+    uint32_t col[CH];
+    float w[CH][8], dw[CH][8];
+    const Row w_row = row_of(a.weight, a.w_f32, 0, n);
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        col[j] = (((uint32_t)j * WPR + sub) * 64u + lane) * 8u;
+        Raw8 r;
+        load8(r, w_row, a.w_f32, col[j]);
+        if ((n & 7u) != 0u) load_tail(r, w_row, a.w_f32, tail_of(col[j], n));
+        values8(r, a.w_f32, w[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
+    }
+    uint32_t turn = 0u;
+    for (uint32_t row0 = blockIdx.x * RPB; row0 < a.rows; row0 += gridDim.x * RPB, turn ^= 1u) {     // the same trips for every wave: they meet
+        const uint32_t row = row0 + slot;
+        const bool in = row < a.rows;
+        const uint32_t n_in = in ? n : 0u;
+        const Row dy_row = row_of(a.dy, false, (size_t)row * a.lddy, n_in), h_row = row_of(a.h, a.h_f32, (size_t)row * a.ldh, n_in);
+        const Row dh_row = row_of(a.dh, a.h_f32, (size_t)row * a.lddh, a.dh ? n_in : 0u);
+        Raw8 rdy[CH], rh[CH], rd[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            load8(rdy[j], dy_row, false, col[j]);
+            load8(rh[j], h_row, a.h_f32, col[j]);
+        }
+        if (a.dh) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) load8(rd[j], dh_row, a.h_f32, col[j]);
+        }
+        if ((n & 7u) != 0u) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const uint32_t tail = in ? tail_of(col[j], n) : 0u;
+                load_tail(rdy[j], dy_row, false, tail);
+                load_tail(rh[j], h_row, a.h_f32, tail);
+                if (a.dh) load_tail(rd[j], dh_row, a.h_f32, tail);
+            }
+        }
+        const float r = in ? a.rstd[row] : 0.0f;
+        float part = 0.0f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float dy[8], h[8];
+            values8(rdy[j], false, dy);
+            values8(rh[j], a.h_f32, h);
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                t[i] = dy[i] * w[j][i] * h[i];
+                dw[j][i] = __builtin_fmaf(dy[i] * r, h[i], dw[j][i]);
+            }
+            part += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        }
+        const float c = row_sum<WPR>(part, meet[turn], slot, sub, lane) / (float)n * r * r;
+        if (a.dx) {
+            const Row dx_row = row_of(a.dx, a.h_f32, (size_t)row * a.lddx, n_in), dx16_row = row_of(a.dx16, false, (size_t)row * a.lddx16, a.dx16 ? n_in : 0u);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const uint32_t tail = in ? tail_of(col[j], n) : 0u;
+                float dy[8], h[8], d[8];
+                values8(rdy[j], false, dy);
+                values8(rh[j], a.h_f32, h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = r * (dy[i] * w[j][i] - h[i] * c);
+                if (a.dh) {
+                    float s[8];
+                    values8(rd[j], a.h_f32, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] += s[i];
+                }
+                store8(dx_row, a.h_f32, col[j], tail, d);
+                if (a.dx16) store8(dx16_row, false, col[j], tail, d);
+            }
+        }
+    }
+    if (!a.partial) return;
+    const uint32_t pitch = (n + 7u) & ~7u;             // whole chunks
+    const Row p_row = row_of(a.partial, true, (size_t)blockIdx.x * pitch, pitch);
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        if (RPB > 1) {
+            __syncthreads();
+            float4* mine = &join[(slot * WPR + sub) * 128u + lane];
+            mine[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+            mine[64] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+            __syncthreads();
+            if (slot == 0u) {
+#pragma unroll
+                for (uint32_t o = 1; o < RPB; ++o) {
+                    const float4 p = join[(o * WPR + sub) * 128u + lane], q = join[(o * WPR + sub) * 128u + 64u + lane];
+                    dw[j][0] += p.x; dw[j][1] += p.y; dw[j][2] += p.z; dw[j][3] += p.w;
+                    dw[j][4] += q.x; dw[j][5] += q.y; dw[j][6] += q.z; dw[j][7] += q.w;
+                }
+            }
+        }
+        if (slot == 0u) store8(p_row, true, col[j], 0u, dw[j]);
+    }
+}
+
+}  // namespace
+
+// out[j] = sum of rows of `partial` [rows x pitch], in order within each of the block's 16 slices, the slices' sums in order
+__global__ void __launch_bounds__(1024)
+column_sum_kernel(const float* __restrict__ partial, uint32_t rows, uint32_t pitch, uint32_t n, float* __restrict__ out) {
+    __shared__ float meet[16][64];
+    const uint32_t lane = threadIdx.x & 63u, slice = threadIdx.x >> 6, c = blockIdx.x * 64u + lane;
+    float s = 0.0f;
+    if (c < n) {
+#pragma unroll 8
+        for (uint32_t r = slice; r < rows; r += 16u) s += partial[(size_t)r * pitch + c];
+    }
+    meet[slice][lane] = s;
+    __syncthreads();
+    if (slice == 0u && c < n) {
+        for (uint32_t i = 1; i < 16u; ++i) s += meet[i][lane];
+        out[c] = s;
+    }
+}
+
+hipError_t launch_column_sum(const float* partial, uint32_t rows, uint32_t pitch, uint32_t n, float* out, hipStream_t st) {
+    hipLaunchKernelGGL(column_sum_kernel, dim3((n + 63u) / 64u), dim3(1024), 0, st, partial, rows, pitch, n, out);
+    return hipGetLastError();
+}
+
+namespace {
+
+// Waves per row and chunks per lane: as few waves as hold a row in four chunks, and more while the rows alone do not give the chip eight waves per
+// compute unit.
+struct NormShape {
+    int wpr, ch;
+};
+NormShape norm_shape(int64_t rows, int64_t n, int most_ch) {
+    const int64_t units = (n + 511) / 512;
+    int wpr = 1;
+    while (wpr < 16 && (int64_t)wpr * most_ch < units) wpr *= 2;
+    while (wpr < 16 && wpr < units && rows * wpr < 2048) wpr *= 2;
+    int ch = 1;
+    while ((int64_t)wpr * ch < units) ch *= 2;
+    return {wpr, ch};
+}
+uint32_t rows_per_block(int wpr) { return wpr < 4 ? 4u / (uint32_t)wpr : 1u; }
+
+template <int WPR, int CH>
+void launch_fwd(const NormFwdArgs& a, int format, hipStream_t st) {
+    const dim3 grid((a.rows + rows_per_block(WPR) - 1u) / rows_per_block(WPR)), block(WPR < 4 ? 256 : 64 * WPR);
+    if (format == kFmtMx4) hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtMx4>), grid, block, 0, st, a);
+    else if (format == kFmtMx8) hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtMx8>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtNone>), grid, block, 0, st, a);
+}
+
+constexpr uint32_t kNormBlocks = 1024;      // blocks of a backward pass: partial sums of the weight's gradient
+uint32_t bwd_blocks(int64_t rows, int64_t n) {
+    const uint32_t rpb = rows_per_block(norm_shape(rows, n, 2).wpr);
+    const int64_t all = (rows + rpb - 1) / rpb;
+    return (uint32_t)(all < kNormBlocks ? all : kNormBlocks);
+}
+
+}  // namespace
+
+#define NORM_SHAPES(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(2, 4) X(4, 1) X(4, 2) X(4, 4) X(8, 1) X(8, 2) X(8, 4) X(16, 1) X(16, 2) X(16, 4)
+
+hipError_t launch_rmsnorm_fwd(const NormFwdArgs& a, int format, hipStream_t st) {
+    if (a.rows == 0) return hipSuccess;
+    const NormShape s = norm_shape(a.rows, a.n, 4);
+#define NORM_CASE(W, C) if (s.wpr == W && s.ch == C) launch_fwd<W, C>(a, format, st);
+    NORM_SHAPES(NORM_CASE)
+#undef NORM_CASE
+    return hipGetLastError();
+}
+
+size_t rmsnorm_bwd_workspace(int64_t rows, int64_t n) { return (size_t)bwd_blocks(rows, n) * (size_t)((n + 7) / 8 * 8) * sizeof(float); }
+
+hipError_t launch_rmsnorm_bwd(const NormBwdArgs& args, float* dweight, float* workspace, hipStream_t st) {
+    if (args.rows == 0) {
+        if (!dweight) return hipSuccess;
+        return launch_column_sum(nullptr, 0u, 0u, args.n, dweight, st);
+    }
+    NormBwdArgs a = args;
+    a.partial = dweight ? workspace : nullptr;
+    const NormShape s = norm_shape(a.rows, a.n, 2);
+    const uint32_t blocks = bwd_blocks(a.rows, a.n);
+#define NORM_CASE(W, C) \
+    if (s.wpr == W && s.ch == C) hipLaunchKernelGGL((rmsnorm_bwd_kernel<W, C>), dim3(blocks), dim3(W < 4 ? 256 : 64 * W), 0, st, a);
+    NORM_SHAPES(NORM_CASE)
+#undef NORM_CASE
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !dweight) return e;
+    return launch_column_sum(workspace, blocks, (a.n + 7u) & ~7u, a.n, dweight, st);
+}
+
+}  // namespace quartet

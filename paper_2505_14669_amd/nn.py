@@ -6,10 +6,16 @@ graph.  There is no fallback: without a GPU or without the built library these c
 
 Shapes: the flattened token count, in_features and out_features must be multiples of the Hadamard
 block (32, the MXFP4 group, unless a layer asks for 64, 128 or 256).
+
+Around the layer, over include/quartet_block.h: an activation, a gate and a residual in the product's epilogue
+(QuartetLinear(activation=...), multiplier=, residual=), the norm of the residual stream (QuartetRMSNorm) and the
+clipping of a step's gradients (clip_grad_norm_).
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as q
+from . import block
 from . import _nn_native as _native          # fails loudly if it has not been built (python -m paper_2505_14669_amd.build)
 
 _native.set_error(q.QuartetError)
@@ -44,15 +50,130 @@ class QuartetLinearFunction:
         return _PythonFunction.apply(*call) if y is None else y
 
 
+def _dtype_code(t):
+    return q.QUARTET_DTYPE_F32 if t is None or t.dtype == torch.float32 else q.QUARTET_DTYPE_BF16
+
+
+def _rows(t, n):
+    """a tensor [..., n] as dense rows whose distance is a multiple of 8 (the kernels' 16-byte accesses), and that distance"""
+    t = t.reshape(-1, n)
+    if n % 8:
+        wide = torch.empty((t.shape[0], n + 8 - n % 8), dtype=t.dtype, device=t.device)
+        wide[:, :n] = t
+        return wide, wide.shape[1]
+    return t.contiguous(), n
+
+
+def _new_rows(rows, n, dtype, device):
+    return torch.empty((rows, n + -n % 8), dtype=dtype, device=device)
+
+
+def _as(t, n, like):
+    return None if t is None else t[:, :n].reshape(like.shape)
+
+
+def _check_tensor(t, name, dtypes, device):
+    if not t.is_cuda or t.device != device:
+        raise RuntimeError(f"{name} must be on {device}: there is no CPU path")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+
+
+_ANY = (torch.bfloat16, torch.float32)
+
+
+class _EpilogueFunction(torch.autograd.Function):
+    """a(x W^T + bias) * multiplier + residual: the layer's operands, its product with the epilogue, and both backward passes."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, multiplier, residual, seed, rounding, hadamard_block, activation):
+        device = x.device
+        _check_tensor(x, "x", (torch.bfloat16,), device)
+        _check_tensor(weight, "weight", (torch.bfloat16,), device)
+        if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1]:
+            raise ValueError("x [..., in_features] and weight [out_features, in_features] do not fit together")
+        out, inf = weight.shape
+        if hadamard_block not in (32, 64, 128, 256):
+            raise ValueError("hadamard_block must be 32, 64, 128 or 256")
+        tokens = x.numel() // inf if inf else 0
+        if tokens % hadamard_block or inf % hadamard_block or out % hadamard_block:
+            raise ValueError(f"tokens, in_features and out_features must be multiples of {hadamard_block}")
+        shape = (*x.shape[:-1], out)
+        for name, t, dtypes in (("multiplier", multiplier, (torch.bfloat16,)), ("residual", residual, _ANY)):
+            if t is not None:
+                _check_tensor(t, name, dtypes, device)
+                if tuple(t.shape) != shape:
+                    raise ValueError(f"{name} must have the result's shape {tuple(shape)}")
+        if bias is not None:
+            _check_tensor(bias, "bias", _ANY, device)
+            if tuple(bias.shape) != (out,):
+                raise ValueError(f"bias must have {out} values")
+        with torch.cuda.device(device):
+            x2, w2 = x.reshape(tokens, inf).contiguous(), weight.contiguous()
+            bias2, mul2, res2 = (None if t is None else t.contiguous() for t in (bias, multiplier, residual))
+            byte = dict(dtype=torch.uint8, device=device)
+            operands = []
+            for t, rows in ((x2, tokens), (w2, out)):
+                operands += [torch.empty(max(16, rows * inf // 2), **byte), torch.empty(max(16, q.quartet_scale_bytes(rows, inf)), **byte),
+                             torch.empty(max(16, rows * inf // 8), **byte)]
+            if hadamard_block == 32:
+                q.check(q.quartet_fwd_operands(x2, w2, tokens, inf, out, *operands))
+            else:
+                q.check(q.quartet_quant_fwd_block(x2, tokens, inf, inf, 0, hadamard_block, *operands[:3]))
+                q.check(q.quartet_quant_fwd_block(w2, out, inf, inf, 0, hadamard_block, *operands[3:]))
+            track = any(ctx.needs_input_grad)
+            pre = torch.empty((tokens, out), dtype=torch.bfloat16, device=device) if track and (activation or mul2 is not None) else None
+            y = torch.empty(shape, dtype=torch.bfloat16 if residual is None else residual.dtype, device=device)
+            q.check(block.quartet_mxfp4_gemm_act(operands[0], operands[1], operands[3], operands[4], tokens, out, inf, 1.0, bias2, _dtype_code(bias2),
+                                                 activation, mul2, out, res2, _dtype_code(res2), out, pre, out, y, _dtype_code(y), out))
+        ctx.save_for_backward(pre, mul2, *operands)
+        ctx.call = (tokens, inf, out, seed, rounding, hadamard_block, activation)
+        ctx.like = (x.shape, None if bias is None else bias.dtype, None if residual is None else residual.dtype)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        pre, mul, *operands = ctx.saved_tensors
+        tokens, inf, out, seed, rounding, hadamard_block, activation = ctx.call
+        x_shape, bias_dtype, residual_dtype = ctx.like
+        device, need = dy.device, ctx.needs_input_grad
+        dx = dw = dbias = dmul = None
+        with torch.cuda.device(device):
+            dz = dy2 = dy.reshape(tokens, out).to(torch.bfloat16).contiguous()
+            if pre is not None or need[2]:
+                plain = activation == 0 and mul is None
+                dz = dy2 if plain else torch.empty_like(dy2)
+                dmul = torch.empty(dy.shape, dtype=torch.bfloat16, device=device) if need[3] else None
+                dbias = torch.empty(out, dtype=torch.float32, device=device) if need[2] else None
+                size = block.quartet_act_bwd_workspace_bytes(tokens, out)
+                ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
+                if dbias is not None or dmul is not None or not plain:
+                    q.check(block.quartet_act_bwd(dy2, out, pre, out, mul, out, tokens, out, activation, None if plain else dz, out, dmul, out, dbias,
+                                                  ws, size))
+            if need[0] or need[1]:
+                dx = torch.empty(x_shape, dtype=torch.bfloat16, device=device)
+                dw = torch.empty((out, inf), dtype=torch.bfloat16, device=device)
+                size = q.quartet_linear_workspace_bytes_block(tokens, inf, out, hadamard_block)
+                ws = torch.empty(max(256, size), dtype=torch.uint8, device=device)
+                q.check(q.quartet_linear_bwd_block(dz, tokens, inf, out, hadamard_block, *operands, seed, rounding, dx, dw, q.QUARTET_DTYPE_BF16, ws, size))
+        return (dx, dw, None if dbias is None else dbias.to(bias_dtype), dmul, dy.to(residual_dtype) if need[4] else None, None, None, None, None)
+
+
 class QuartetLinear(torch.nn.Module):
     """nn.Linear replacement: weight [out, in] (bf16, or fp32 master weights cast to bf16 on the way
-    in), optional bf16 bias added outside the quantized product.  Every backward pass uses a fresh stochastic-rounding seed: base seed, layer id and a
+    in), optional bf16 bias.  activation ("none", "relu", "gelu", "silu"), multiplier (bf16, the other branch of a gated layer) and
+    residual (bf16 or fp32, whose type the result then has) join the product's epilogue: a(x W^T + bias) * multiplier + residual; without
+    any of them the bias is added to the product's bf16 result.  Every backward pass uses a fresh stochastic-rounding seed: base seed, layer id and a
     per-layer call counter packed into 64 bits, so runs are reproducible and no two calls share draws."""
     _next_id = 0
 
     def __init__(self, in_features, out_features, bias=False, seed=0, rounding=0, device="cuda",
-                 weight_dtype=torch.bfloat16, hadamard_block=32):
+                 weight_dtype=torch.bfloat16, hadamard_block=32, activation="none"):
         super().__init__()
+        if activation not in block.ACTIVATIONS:
+            raise ValueError(f"activation must be one of {', '.join(block.ACTIVATIONS)}")
+        self.activation = activation
         self.hadamard_block = hadamard_block
         self.in_features, self.out_features = in_features, out_features
         w = torch.randn(out_features, in_features, device=device) * (in_features ** -0.5)
@@ -65,8 +186,108 @@ class QuartetLinear(torch.nn.Module):
         QuartetLinear._next_id += 1
         self.calls = 0
 
-    def forward(self, x):
+    def forward(self, x, multiplier=None, residual=None):
         seed = (self.base_seed << 48) | (self.layer_id << 32) | (self.calls & 0xFFFFFFFF)
         self.calls += 1
-        y = QuartetLinearFunction.apply(x, self.weight.to(torch.bfloat16), seed, self.rounding, self.hadamard_block)
+        weight = self.weight.to(torch.bfloat16)
+        if self.activation != "none" or multiplier is not None or residual is not None:
+            return _EpilogueFunction.apply(x, weight, self.bias, multiplier, residual, seed, self.rounding, self.hadamard_block,
+                                           block.ACTIVATIONS[self.activation])
+        y = QuartetLinearFunction.apply(x, weight, seed, self.rounding, self.hadamard_block)
         return y if self.bias is None else y + self.bias
+
+
+class _RMSNormFunction(torch.autograd.Function):
+    """(y, h) of the norm over x, or over h = residual + x"""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        device = x.device
+        n = weight.numel()
+        _check_tensor(x, "x", _ANY, device)
+        _check_tensor(weight, "weight", _ANY, device)
+        if weight.dim() != 1 or n < 1 or x.dim() < 1 or x.shape[-1] != n:
+            raise ValueError("x [..., n] and weight [n] do not fit together")
+        if residual is not None:
+            _check_tensor(residual, "residual", _ANY, device)
+            if residual.shape != x.shape:
+                raise ValueError("residual must have the shape of x")
+        rows = x.numel() // n
+        with torch.cuda.device(device):
+            x2, ld = _rows(x, n)
+            res2 = None if residual is None else _rows(residual, n)[0]
+            w2 = weight.contiguous()
+            h2 = None if residual is None else _new_rows(rows, n, residual.dtype, device)
+            y2, rstd = _new_rows(rows, n, torch.bfloat16, device), torch.empty(rows, dtype=torch.float32, device=device)
+            if rows:
+                q.check(block.quartet_rmsnorm_fwd(x2, _dtype_code(x2), ld, res2, ld, rows, n, w2, _dtype_code(w2), float(eps), h2, _dtype_code(h2),
+                                                  ld, y2, ld, block.QUARTET_FORMAT_NONE, None, None, None, rstd))
+        ctx.save_for_backward(x2 if h2 is None else h2, w2, rstd)
+        ctx.like = (x.shape, x.dtype, None if residual is None else residual.dtype, rows, n, ld)
+        ctx.set_materialize_grads(False)
+        y = _as(y2, n, x)
+        return y, (None if h2 is None else _as(h2, n, x))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        h, w, rstd = ctx.saved_tensors
+        shape, x_dtype, residual_dtype, rows, n, ld = ctx.like
+        if dy is None:
+            return (None if dh is None else dh.to(x_dtype)), dh, None, None
+        need, device = ctx.needs_input_grad, h.device
+        with torch.cuda.device(device):
+            dy2 = _rows(dy.to(torch.bfloat16), n)[0]
+            dh2 = None if dh is None else _rows(dh.to(h.dtype), n)[0]
+            wants_x = need[0] or need[1]
+            dx = _new_rows(rows, n, h.dtype, device) if wants_x else None
+            dx16 = _new_rows(rows, n, torch.bfloat16, device) if wants_x and h.dtype == torch.float32 and x_dtype == torch.bfloat16 else None
+            dw = (torch.empty if rows else torch.zeros)(n, dtype=torch.float32, device=device) if need[2] else None
+            size = block.quartet_rmsnorm_bwd_workspace_bytes(rows, n)
+            ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
+            if rows and (wants_x or need[2]):
+                q.check(block.quartet_rmsnorm_bwd(dy2, ld, h, _dtype_code(h), ld, rows, n, w, _dtype_code(w), rstd, dh2, ld, dx, ld, dx16, ld, dw, ws, size))
+        like = dy
+        gx = _as(dx16 if dx16 is not None else dx, n, like) if need[0] else None
+        return (None if gx is None else gx.to(x_dtype), _as(dx, n, like) if need[1] else None, None if dw is None else dw.to(w.dtype), None)
+
+
+class QuartetRMSNorm(torch.nn.Module):
+    """y = h / sqrt(mean(h^2) + eps) * weight as bf16, what QuartetLinear takes.  forward(x): h = x.  forward(x, residual): h = residual + x in
+    residual's type, and the result is (y, h): the norm and the stream it leaves for the next layer.  x, residual [..., n] bf16 or fp32."""
+
+    def __init__(self, n, eps=1e-5, device="cuda", weight_dtype=torch.float32):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(n, dtype=weight_dtype, device=device))
+        self.eps = eps
+
+    def forward(self, x, residual=None):
+        y, h = _RMSNormFunction.apply(x, residual, self.weight, self.eps)
+        return y if residual is None else (y, h)
+
+
+def _in_storage_order(g):
+    """a dense gradient as it lies in memory"""
+    v = g.permute(sorted(range(g.dim()), key=lambda d: (-g.stride(d), d))) if g.dim() > 1 and not g.is_contiguous() else g
+    if not v.is_contiguous():
+        raise q.QuartetError("gradients must be dense")
+    return v
+
+
+@torch.no_grad()
+def clip_grad_norm_(parameters, max_norm):
+    """Scales the gradients of `parameters` (bf16 or fp32, on one GPU) in place so that their common norm is at most max_norm, and returns
+    the norm they had, on the device.  Two launches for 80 tensors, no synchronization.  A norm that is not finite leaves the gradients as they are."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
+    grads = [_in_storage_order(p.grad) for p in {id(p): p for p in parameters}.values() if p.grad is not None]
+    if not grads:
+        return torch.zeros((), device=parameters[0].device if parameters else None)
+    device = grads[0].device
+    if any(g.device != device for g in grads):
+        raise q.QuartetError("all gradients must be on one GPU")
+    with torch.cuda.device(device):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        size = block.quartet_grad_clip_workspace_bytes()
+        tensors = block.grad_tensors(grads)
+        q.check(block.quartet_grad_clip(tensors, len(tensors), float(max_norm), norm, torch.empty(size, dtype=torch.uint8, device=device), size))
+    return norm
