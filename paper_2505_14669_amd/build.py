@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libquartet.so")
 NN_LIB = os.path.join(HERE, "_nn_native" + sysconfig.get_config_var("EXT_SUFFIX"))     # another Python does not take it for its own
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "quant_kernels.hip", "gemm_kernels.hip", "gemm_split_kernels.hip", "epilogue_kernels.hip", "fp8_kernels.hip", "probe_kernels.hip",
-           "api_block.hip", "norm_kernels.hip", "act_kernels.hip", "clip_kernels.hip"]
+           "gemm_act_kernels.hip", "api_block.hip", "norm_kernels.hip", "act_kernels.hip", "clip_kernels.hip"]
 
 # -ffp-contract=off: the Hadamard butterflies and scale arithmetic must not be fused into FMAs;
 # packed-fp32 VALU ops are disabled (they have given wrong results on these machines).

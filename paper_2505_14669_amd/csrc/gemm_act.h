@@ -97,4 +97,168 @@ __device__ __forceinline__ void store_act_chunk(void* d, uint32_t ld, uint32_t r
     }
 }
 
+// A matrix's part of a wave's tile: a buffer resource that ends with the matrix's last element in these rows, so rows past the matrix are neither read
+// nor written without a predicate; a lane whose columns lie outside takes an offset that no resource reaches.
+struct ActTile {
+    __amdgpu_buffer_rsrc_t res;
+    uint32_t row_bytes;
+};
+__device__ __forceinline__ ActTile act_tile(const void* p, uint32_t size, uint32_t ld, uint32_t row_base, uint32_t rows, uint32_t n) {
+    const size_t row_bytes = (size_t)ld * size;
+    return {make_rsrc(static_cast<const uint8_t*>(p) + row_base * row_bytes, p && rows ? (rows - 1u) * (uint32_t)row_bytes + n * size : 0u), (uint32_t)row_bytes};
+}
+constexpr int kThroughL2 = 16;      // cache policy of a buffer store: sc1, as store_through16
+
+// Epilogue of the streaming kernels for quartet_mxfp4_gemm_act: the wave's accumulator tile leaves in passes of eight rows through its scratch as in
+// store_tile_rows8 (same image in LDS, same chunk of four columns of every 32-column slice in a lane), and every chunk takes its bias, goes through the
+// activation and meets its gate and residual.  Those are loaded DEPTH passes ahead, in the order of the passes between their stores: the
+// vector-memory counter retires in order, so what a pass waits for is older than the stores of the passes in between.  Loads and stores here are builtins:
+// the compiler counts them and waits for the right ones (it would wait for every store of the preceding passes if it did not see them).  The ring's loads
+// are older than all of it.
+// Whether every store was issued: TM * 4 * TN of results, what the kernels' first barrier behind a tile counts on.
+template <int TM, int TN, int DEPTH, bool OUT_BF16, typename ACC, int AM, int AN>
+__device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, void* d, uint32_t ldd, float alpha, uint32_t row_base, uint32_t col_base,
+                                               uint32_t m, uint32_t n, uint32_t lane, const GemmActArgs& e) {
+    static_assert(TN == 2 || TN == 4, "the slice swap of odd rows pairs the slices up");
+    constexpr bool A32 = sizeof(ACC) == sizeof(v16f);
+    static_assert(AM == (A32 ? TM : 2 * TM) && AN == (A32 ? TN : 2 * TN), "the accumulators must make up the tile");
+    constexpr uint32_t PASSES = TM * 4, W = TN * 32;
+    const uint32_t sub = lane >> 3, c = lane & 7u;
+    const uint32_t lhalf = lane >> 5, wq = lane >> 4;
+    float* wr = wbuf + lhalf * 4u * W + (lane & 31u);
+    float* wr_even = wbuf + 2u * wq * W + (lane & 15u) + (wq & 1u) * 16u;
+    float* wr_odd = wbuf + 2u * wq * W + (lane & 15u) - (wq & 1u) * 16u;
+    const uint32_t rswz = A32 ? (sub ^ (sub >> 2)) & 1u : sub & 1u;
+    const float* rd = wbuf + sub * W + 4u * (A32 ? c : c ^ (((sub >> 1) & 1u) * 4u));
+    const uint32_t row_in_tile = A32 ? sub : 4u * (sub >> 1) + (sub & 1u);
+    auto row_step = [](uint32_t p) { return A32 ? p * 8u : (p >> 1) * 16u + (p & 1u) * 2u; };
+    auto write_pass = [&](uint32_t p) __attribute__((always_inline)) {
+        if constexpr (A32) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j)
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t) wr[t * W + ((j ^ ((t & 1u) ^ lhalf)) * 32u)] = acc[p >> 2][j][(p & 3u) * 4u + t];
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 2u * TN; ++j)
+#pragma unroll
+                for (uint32_t t = 0; t < 2; ++t) ((j & 1u) ? wr_odd : wr_even)[t * W + (j ^ (2u * t)) * 16u] = acc[p >> 1][j][(p & 1u) * 2u + t];
+        }
+    };
+    const bool whole = (n & 3u) == 0u && act_wide(e, ldd);      // wave-uniform: every chunk lies inside or outside, at a multiple of its size
+    if (!whole) {
+        // one pass after the other, the code of one: only the accumulators have to be named
+#pragma unroll 1
+        for (uint32_t p = 0; p < PASSES; ++p) {
+#pragma unroll
+            for (uint32_t named = 0; named < PASSES; ++named)
+                if (named == p) write_pass(named);
+            float vv[TN][4];
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) {
+                const float4 t = *reinterpret_cast<const float4*>(&rd[(j ^ rswz) * 32u]);
+                vv[j][0] = t.x; vv[j][1] = t.y; vv[j][2] = t.z; vv[j][3] = t.w;
+            }
+            const uint32_t row = row_base + row_in_tile + row_step(p);
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) {
+                const uint32_t col = col_base + j * 32u + 4u * c;
+                ActChunk extra;
+                float bias[4];
+                load_act_chunk(extra, e, row, col, m, n, false);
+                load_bias(bias, e, col, n);
+#pragma unroll
+                for (uint32_t t = 0; t < 4; ++t) vv[j][t] = vv[j][t] * alpha + bias[t];
+                if (e.pre) store_act_chunk<true>(e.pre, e.ldpre, row, col, m, n, false, vv[j]);
+                activate(vv[j], e.act);
+                combine_act_chunk(vv[j], extra, e);
+                store_act_chunk<OUT_BF16>(d, ldd, row, col, m, n, false, vv[j]);
+            }
+        }
+        return false;
+    }
+    constexpr uint32_t SD = OUT_BF16 ? 2u : 4u;
+    const uint32_t rows = row_base < m ? (m - row_base < TM * 32u ? m - row_base : TM * 32u) : 0u;
+    const uint32_t sr = e.res_kind == 2 ? 4u : 2u;
+    const ActTile td = act_tile(d, SD, ldd, row_base, rows, n), tr = act_tile(e.residual, sr, e.ldres, row_base, rows, n);
+    const ActTile tm = act_tile(e.mul, 2u, e.ldmul, row_base, rows, n), tp = act_tile(e.pre, 2u, e.ldpre, row_base, rows, n);
+    uint32_t at[TN];                                             // the lane's columns
+    float bias[TN][4];
+#pragma unroll
+    for (uint32_t j = 0; j < TN; ++j) at[j] = col_base + j * 32u + 4u * c;
+    // byte offset of chunk j in the lane's row of pass 0
+    auto place = [&](uint32_t j, uint32_t size, uint32_t row_bytes) { return at[j] < n ? row_in_tile * row_bytes + at[j] * size : kOutOfRange; };
+    if (e.bias_kind == 2) {
+        const __amdgpu_buffer_rsrc_t b = make_rsrc(e.bias, n * 4u);
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) {
+            const v4u_t t = __builtin_amdgcn_raw_buffer_load_b128(b, (int)(at[j] * 4u), 0, 0);
+            bias[j][0] = u2f(t.x); bias[j][1] = u2f(t.y); bias[j][2] = u2f(t.z); bias[j][3] = u2f(t.w);
+        }
+    } else {
+        const __amdgpu_buffer_rsrc_t b = make_rsrc(e.bias, e.bias_kind ? n * 2u : 0u);
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) {
+            const v2u_t t = __builtin_amdgcn_raw_buffer_load_b64(b, (int)(at[j] * 2u), 0, 0);
+            bias[j][0] = bf16_lo(t.x); bias[j][1] = bf16_hi(t.x); bias[j][2] = bf16_lo(t.y); bias[j][3] = bf16_hi(t.y);
+        }
+    }
+    ActChunk extra[DEPTH][TN];
+    auto load_pass = [&](uint32_t p) __attribute__((always_inline)) {
+        ActChunk (&x)[TN] = extra[p % DEPTH];
+        if (e.res_kind == 2) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) x[j].res = __builtin_amdgcn_raw_buffer_load_b128(tr.res, (int)place(j, 4u, tr.row_bytes), (int)(row_step(p) * tr.row_bytes), 0);
+        } else if (e.res_kind == 1) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) {
+                const v2u_t t = __builtin_amdgcn_raw_buffer_load_b64(tr.res, (int)place(j, 2u, tr.row_bytes), (int)(row_step(p) * tr.row_bytes), 0);
+                x[j].res.x = t.x; x[j].res.y = t.y;
+            }
+        }
+        if (e.mul) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) x[j].mul = __builtin_amdgcn_raw_buffer_load_b64(tm.res, (int)place(j, 2u, tm.row_bytes), (int)(row_step(p) * tm.row_bytes), 0);
+        }
+    };
+#pragma unroll
+    for (uint32_t p = 0; p < DEPTH; ++p) load_pass(p);
+    write_pass(0u);
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES; ++p) {
+        float vv[TN * 4];
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) {
+            const float4 t = *reinterpret_cast<const float4*>(&rd[(j ^ rswz) * 32u]);
+            vv[4 * j] = t.x; vv[4 * j + 1] = t.y; vv[4 * j + 2] = t.z; vv[4 * j + 3] = t.w;
+        }
+        if (p + 1u < PASSES) write_pass(p + 1u);      // behind the reads in the wave's LDS queue
+#pragma unroll
+        for (uint32_t t = 0; t < 4u * TN; ++t) vv[t] = vv[t] * alpha + bias[t >> 2][t & 3u];
+        if (e.pre) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j) {
+                const v2u_t z = {bf16_pack2(vv[4 * j], vv[4 * j + 1]), bf16_pack2(vv[4 * j + 2], vv[4 * j + 3])};
+                __builtin_amdgcn_raw_buffer_store_b64(z, tp.res, (int)place(j, 2u, tp.row_bytes), (int)(row_step(p) * tp.row_bytes), kThroughL2);
+            }
+        }
+        activate(vv, e.act);
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) combine_act_chunk(reinterpret_cast<float (&)[4]>(vv[4 * j]), extra[p % DEPTH][j], e);
+        if (p + DEPTH < PASSES) load_pass(p + DEPTH);
+#pragma unroll
+        for (uint32_t j = 0; j < TN; ++j) {
+            const int voff = (int)place(j, SD, td.row_bytes), soff = (int)(row_step(p) * td.row_bytes);
+            if (OUT_BF16) {
+                const v2u_t o = {bf16_pack2(vv[4 * j], vv[4 * j + 1]), bf16_pack2(vv[4 * j + 2], vv[4 * j + 3])};
+                __builtin_amdgcn_raw_buffer_store_b64(o, td.res, voff, soff, kThroughL2);
+            } else {
+                const v4u_t o = {f2u(vv[4 * j]), f2u(vv[4 * j + 1]), f2u(vv[4 * j + 2]), f2u(vv[4 * j + 3])};
+                __builtin_amdgcn_raw_buffer_store_b128(o, td.res, voff, soff, kThroughL2);
+            }
+        }
+    }
+    return true;
+}
+
 }  // namespace quartet
