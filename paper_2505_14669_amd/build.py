@@ -11,8 +11,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libquartet.so")
 NN_LIB = os.path.join(HERE, "_nn_native" + sysconfig.get_config_var("EXT_SUFFIX"))     # another Python does not take it for its own
 OBJDIR = os.path.join(HERE, "_build")
-SOURCES = ["api.hip", "quant_kernels.hip", "gemm_kernels.hip", "gemm_split_kernels.hip", "epilogue_kernels.hip", "fp8_kernels.hip", "probe_kernels.hip",
-           "gemm_act_kernels.hip", "api_block.hip", "norm_kernels.hip", "act_kernels.hip", "clip_kernels.hip"]
+SOURCES = ["gemm_act_bf16_kernels.hip", "gemm_act_f32_kernels.hip", "api.hip", "quant_kernels.hip", "gemm_kernels.hip",
+           "gemm_split_kernels.hip", "epilogue_kernels.hip", "fp8_kernels.hip", "probe_kernels.hip",
+           "api_block.hip", "norm_kernels.hip", "act_kernels.hip", "clip_kernels.hip"]
 
 # -ffp-contract=off: the Hadamard butterflies and scale arithmetic must not be fused into FMAs;
 # packed-fp32 VALU ops are disabled (they have given wrong results on these machines).
@@ -60,7 +61,7 @@ def build(verbose=False):
     """Returns the library's path.  The library needs hipcc alone and is linked whatever becomes of the torch node; without torch, which
     the node's only user imports as well, there is no node."""
     os.makedirs(OBJDIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=5) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         nn = ex.submit(_compile_nn) if _have_torch() else None
         results = list(ex.map(_compile, SOURCES))
     if verbose:

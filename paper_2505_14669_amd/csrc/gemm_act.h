@@ -107,6 +107,7 @@ __device__ __forceinline__ ActTile act_tile(const void* p, uint32_t size, uint32
     const size_t row_bytes = (size_t)ld * size;
     return {make_rsrc(static_cast<const uint8_t*>(p) + row_base * row_bytes, p && rows ? (rows - 1u) * (uint32_t)row_bytes + n * size : 0u), (uint32_t)row_bytes};
 }
+enum ActExtra { kExtraNone, kExtraOne, kExtraFp32, kExtraBoth };
 constexpr int kThroughL2 = 16;      // cache policy of a buffer store: sc1, as store_through16
 
 // Epilogue of the streaming kernels for quartet_mxfp4_gemm_act: the wave's accumulator tile leaves in passes of eight rows through its scratch as in
@@ -116,7 +117,9 @@ constexpr int kThroughL2 = 16;      // cache policy of a buffer store: sc1, as s
 // the compiler counts them and waits for the right ones (it would wait for every store of the preceding passes if it did not see them).  The ring's loads
 // are older than all of it.
 // Whether every store was issued: TM * 4 * TN of results, what the kernels' first barrier behind a tile counts on.
-template <int TM, int TN, int DEPTH, bool OUT_BF16, typename ACC, int AM, int AN>
+// EXTRA: what a chunk meets, so that no register is kept for what does not exist: nothing, one bf16 matrix (gate or residual), an fp32 residual, or a gate and a
+// residual of either type.
+template <int TM, int TN, int EXTRA, int DEPTH, bool OUT_BF16, typename ACC, int AM, int AN>
 __device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, void* d, uint32_t ldd, float alpha, uint32_t row_base, uint32_t col_base,
                                                uint32_t m, uint32_t n, uint32_t lane, const GemmActArgs& e) {
     static_assert(TN == 2 || TN == 4, "the slice swap of odd rows pairs the slices up");
@@ -175,13 +178,17 @@ __device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, 
                 store_act_chunk<OUT_BF16>(d, ldd, row, col, m, n, false, vv[j]);
             }
         }
+        __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0), said here: otherwise the compiler, not sure of every branch's loads, says it in the main loop
         return false;
     }
     constexpr uint32_t SD = OUT_BF16 ? 2u : 4u;
     const uint32_t rows = row_base < m ? (m - row_base < TM * 32u ? m - row_base : TM * 32u) : 0u;
+    // EXTRA = one bf16 matrix: `one` of them, otherwise the residual and the gate
+    const bool gates = EXTRA == kExtraOne && e.mul != nullptr;
     const uint32_t sr = e.res_kind == 2 ? 4u : 2u;
-    const ActTile td = act_tile(d, SD, ldd, row_base, rows, n), tr = act_tile(e.residual, sr, e.ldres, row_base, rows, n);
-    const ActTile tm = act_tile(e.mul, 2u, e.ldmul, row_base, rows, n), tp = act_tile(e.pre, 2u, e.ldpre, row_base, rows, n);
+    const ActTile td = act_tile(d, SD, ldd, row_base, rows, n), tp = act_tile(e.pre, 2u, e.ldpre, row_base, rows, n);
+    const ActTile tr = act_tile(gates ? e.mul : e.residual, gates ? 2u : sr, gates ? e.ldmul : e.ldres, row_base, rows, n);
+    const ActTile tm = act_tile(EXTRA == kExtraBoth ? e.mul : nullptr, 2u, e.ldmul, row_base, rows, n);
     uint32_t at[TN];                                             // the lane's columns
     float bias[TN][4];
 #pragma unroll
@@ -203,26 +210,55 @@ __device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, 
             bias[j][0] = bf16_lo(t.x); bias[j][1] = bf16_hi(t.x); bias[j][2] = bf16_lo(t.y); bias[j][3] = bf16_hi(t.y);
         }
     }
-    ActChunk extra[DEPTH][TN];
+    constexpr int D = EXTRA == kExtraNone ? 1 : DEPTH;
+    v2u_t one[D][TN], gate[D][TN];
+    v4u_t full[D][TN];
     auto load_pass = [&](uint32_t p) __attribute__((always_inline)) {
-        ActChunk (&x)[TN] = extra[p % DEPTH];
-        if (e.res_kind == 2) {
+        const uint32_t s = p % D;
+        const int soff = (int)(row_step(p) * tr.row_bytes);
 #pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) x[j].res = __builtin_amdgcn_raw_buffer_load_b128(tr.res, (int)place(j, 4u, tr.row_bytes), (int)(row_step(p) * tr.row_bytes), 0);
-        } else if (e.res_kind == 1) {
-#pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) {
-                const v2u_t t = __builtin_amdgcn_raw_buffer_load_b64(tr.res, (int)place(j, 2u, tr.row_bytes), (int)(row_step(p) * tr.row_bytes), 0);
-                x[j].res.x = t.x; x[j].res.y = t.y;
+        for (uint32_t j = 0; j < TN; ++j) {
+            if (EXTRA == kExtraOne) one[s][j] = __builtin_amdgcn_raw_buffer_load_b64(tr.res, (int)place(j, 2u, tr.row_bytes), soff, 0);
+            if (EXTRA == kExtraFp32) full[s][j] = __builtin_amdgcn_raw_buffer_load_b128(tr.res, (int)place(j, 4u, tr.row_bytes), soff, 0);
+            if (EXTRA == kExtraBoth) {
+                if (e.res_kind == 2) {
+                    full[s][j] = __builtin_amdgcn_raw_buffer_load_b128(tr.res, (int)place(j, 4u, tr.row_bytes), soff, 0);
+                } else {
+                    const v2u_t t = __builtin_amdgcn_raw_buffer_load_b64(tr.res, (int)place(j, 2u, tr.row_bytes), soff, 0);
+                    full[s][j].x = t.x; full[s][j].y = t.y;
+                }
+                gate[s][j] = __builtin_amdgcn_raw_buffer_load_b64(tm.res, (int)place(j, 2u, tm.row_bytes), (int)(row_step(p) * tm.row_bytes), 0);
             }
         }
-        if (e.mul) {
+    };
+    auto combine = [&](uint32_t p, float* v) __attribute__((always_inline)) {      // v: the pass's 4 TN values
+        const uint32_t s = p % D;
+        if (EXTRA == kExtraOne) {
+            if (gates) {
 #pragma unroll
-            for (uint32_t j = 0; j < TN; ++j) x[j].mul = __builtin_amdgcn_raw_buffer_load_b64(tm.res, (int)place(j, 2u, tm.row_bytes), (int)(row_step(p) * tm.row_bytes), 0);
+                for (uint32_t j = 0; j < TN; ++j, v += 4) {
+                    v[0] *= bf16_lo(one[s][j].x); v[1] *= bf16_hi(one[s][j].x); v[2] *= bf16_lo(one[s][j].y); v[3] *= bf16_hi(one[s][j].y);
+                }
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < TN; ++j, v += 4) {
+                    v[0] += bf16_lo(one[s][j].x); v[1] += bf16_hi(one[s][j].x); v[2] += bf16_lo(one[s][j].y); v[3] += bf16_hi(one[s][j].y);
+                }
+            }
+        }
+        if (EXTRA == kExtraFp32) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j, v += 4) {
+                v[0] += u2f(full[s][j].x); v[1] += u2f(full[s][j].y); v[2] += u2f(full[s][j].z); v[3] += u2f(full[s][j].w);
+            }
+        }
+        if (EXTRA == kExtraBoth) {
+#pragma unroll
+            for (uint32_t j = 0; j < TN; ++j, v += 4) combine_act_chunk(reinterpret_cast<float (&)[4]>(*v), ActChunk{full[s][j], gate[s][j]}, e);
         }
     };
 #pragma unroll
-    for (uint32_t p = 0; p < DEPTH; ++p) load_pass(p);
+    for (uint32_t p = 0; p < D && p < PASSES; ++p) load_pass(p);
     write_pass(0u);
 #pragma unroll
     for (uint32_t p = 0; p < PASSES; ++p) {
@@ -243,9 +279,12 @@ __device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, 
             }
         }
         activate(vv, e.act);
-#pragma unroll
-        for (uint32_t j = 0; j < TN; ++j) combine_act_chunk(reinterpret_cast<float (&)[4]>(vv[4 * j]), extra[p % DEPTH][j], e);
-        if (p + DEPTH < PASSES) load_pass(p + DEPTH);
+        combine(p, vv);
+        if (p + D < PASSES) load_pass(p + D);
+        if (EXTRA != kExtraNone && p + 1u == PASSES) {       // nothing is left of the loads: as above, and free (D passes' stores are younger than the last load)
+            constexpr uint32_t younger = D * TN < 63 ? D * TN : 63;
+            __builtin_amdgcn_s_waitcnt(0x0F70u | (younger & 15u) | ((younger >> 4) << 14));
+        }
 #pragma unroll
         for (uint32_t j = 0; j < TN; ++j) {
             const int voff = (int)place(j, SD, td.row_bytes), soff = (int)(row_step(p) * td.row_bytes);

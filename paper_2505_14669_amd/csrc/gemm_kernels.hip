@@ -384,7 +384,8 @@ hipError_t launch_gemm_act(const GemmArgs& g, const GemmActArgs& act, int d_bf16
     batch.p[1] = GemmProblem{};      // no second product
     batch.past = batch.extra_tiles = batch.late = 0u;
     const uint32_t room = (plan.shape == kTwoPerCu ? 2u : 1u) * (uint32_t)stream_blocks(), total = batch.p[0].total_tiles;
-    return launch_gemm_act_stream(batch, act, d_bf16, plan.shape, total < room ? total : room, st);
+    const uint32_t blocks = total < room ? total : room;
+    return d_bf16 ? launch_gemm_act_stream<true>(batch, act, plan.shape, blocks, st) : launch_gemm_act_stream<false>(batch, act, plan.shape, blocks, st);
 }
 
 }  // namespace quartet

@@ -1,10 +1,15 @@
-// The streaming MXFP4 products: the bodies of the kernels in gemm_kernels.hip (plain results and the gradient epilogue) and gemm_act_kernels.hip (bias,
+// The streaming MXFP4 products: the bodies of the kernels in gemm_kernels.hip (plain results and the gradient epilogue) and gemm_act_kernels.h (bias,
 // activation, gate and residual).  Operand layouts, instruction choice and measurements: gemm_kernels.hip.
 #pragma once
 #include "gemm_act.h"
 #include "gemm_common.h"
 
 namespace quartet {
+
+// Passes of the epilogue that the loads of its operands are ahead (store_tile_act): as many as the registers hold beside the accumulators and the next tile's
+// first fragments.
+constexpr int act_depth_large(int extra) { return extra == kExtraOne ? 8 : extra == kExtraFp32 ? 4 : 2; }
+constexpr int act_depth(int extra, int tn) { return extra == kExtraOne ? 8 : extra == kExtraFp32 ? (tn == 4 ? 4 : 6) : 3; }
 
 // One product of a launch of the streaming kernels, and the one or two products a launch works through: a
 // block walks tiles of the first product, then of the second (TileWalk; Algorithm 1 Backward: the two gradient
@@ -64,8 +69,8 @@ __device__ __forceinline__ uint32_t scale_selector(uint32_t lane, uint32_t group
 // The epilogue uses a scratch of its own (16 KB beside the 136 KB ring).
 // WIDE: Hadamard blocks of 256 columns (store_tile_rows8): sizes are multiples of the tile.  PAST16: bf16 results past the memory-side cache: a
 // branch per pass, as fp32 results have it, costs bf16 launches 0.5-1.6 % (layer step 2336 x 1376 x 3168 58.3 -> 59.2 us).
-// E: none, or GemmActArgs: the epilogue of quartet_mxfp4_gemm_act.
-template <bool OUT_BF16, bool FUSED, bool WIDE, bool PAST16 = false, typename... E>
+// E: none, or GemmActArgs: the epilogue of quartet_mxfp4_gemm_act with what EXTRA says.
+template <bool OUT_BF16, bool FUSED, bool WIDE, bool PAST16 = false, int EXTRA = 0, typename... E>
 __device__ __forceinline__ void stream_large_tiles(const GemmBatch& batch, uint32_t nb, uint64_t* __restrict__ clock_counters, const E&... epilogue) {
     constexpr uint32_t TM = 4, TN = 4, BM = 256, BN = 256;
     constexpr uint32_t CODES = (BM + BN) * 8;            // 16-byte chunks of codes per K-quad
@@ -308,7 +313,7 @@ __device__ __forceinline__ void stream_large_tiles(const GemmBatch& batch, uint3
         const uint32_t* __restrict__ mask = q.mask;
         const uint32_t row_base = m0 + wm0, col_base = n0 + wn0;
         const bool full = (ldd & 3u) == 0u && row_base + TM * 32u <= m && col_base + TN * 32u <= n && (!FUSED || mask != nullptr);
-        if constexpr (sizeof...(E) == 1) stores = (store_tile_act<TM, TN, 2, OUT_BF16>(acc, wbuf, q.d, ldd, q.alpha, row_base, col_base, m, n, lane, epilogue), ...);
+        if constexpr (sizeof...(E) == 1) stores = (store_tile_act<TM, TN, EXTRA, act_depth_large(EXTRA), OUT_BF16>(acc, wbuf, q.d, ldd, q.alpha, row_base, col_base, m, n, lane, epilogue), ...);
         else if constexpr (WIDE) store_tile_rows8<TM, TN, OUT_BF16, FUSED, true, true>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
         else if (full) store_tile_rows8<TM, TN, OUT_BF16, FUSED, true>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
         else store_tile_rows8<TM, TN, OUT_BF16, FUSED, false>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
@@ -354,7 +359,7 @@ __device__ __forceinline__ void stream_large_tiles(const GemmBatch& batch, uint3
 // Pairs of layers (tokens, in, out), one block / two (us): 608 x 8832 x 3424 63.6 / 52.7, 4800 x 1824 x 2112 48.9 / 43.6, 9600 x 576 x 576 32.4 /
 // 36.0 (a tile or two per compute unit: the deeper ring); single products 10327 x 992 x 800 21.1 / 17.9, 4926 x 6496 x 10144 230 / 251.
 // E: as for the 256 x 256 tiles.
-template <int TM, int TN, int PER_CU, bool OUT_BF16, bool FUSED, bool WIDE = false, bool PAST16 = false, typename... E>
+template <int TM, int TN, int PER_CU, bool OUT_BF16, bool FUSED, bool WIDE = false, bool PAST16 = false, int EXTRA = 0, typename... E>
 __device__ __forceinline__ void stream_tiles(const GemmBatch& batch, uint32_t nb, uint64_t* __restrict__ clock_counters, const E&... epilogue) {
     constexpr uint32_t BM = 64 * TM, BN = 64 * TN;
     static_assert(BM % 128 == 0 && BN % 128 == 0, "a wave's four scale tiles must belong to one operand");
@@ -585,7 +590,7 @@ __device__ __forceinline__ void stream_tiles(const GemmBatch& batch, uint32_t nb
         const uint32_t* __restrict__ mask = q.mask;
         const uint32_t row_base = m0 + wm0, col_base = n0 + wn0;
         const bool full = (ldd & 3u) == 0u && row_base + TM * 32u <= m && col_base + TN * 32u <= n && (!FUSED || mask != nullptr);
-        if constexpr (sizeof...(E) == 1) stores = (store_tile_act<TM, TN, 2, OUT_BF16>(acc, wbuf, q.d, ldd, q.alpha, row_base, col_base, m, n, lane, epilogue), ...);
+        if constexpr (sizeof...(E) == 1) stores = (store_tile_act<TM, TN, EXTRA, act_depth(EXTRA, TN), OUT_BF16>(acc, wbuf, q.d, ldd, q.alpha, row_base, col_base, m, n, lane, epilogue), ...);
         else if constexpr (WIDE) store_tile_rows8<TM, TN, OUT_BF16, FUSED, true, true>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
         else if (full) store_tile_rows8<TM, TN, OUT_BF16, FUSED, true>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
         else store_tile_rows8<TM, TN, OUT_BF16, FUSED, false>(acc, wbuf, q.d, ldd, mask, q.alpha, row_base, col_base, m, n, lane, nb, past);
@@ -614,7 +619,8 @@ __device__ __forceinline__ void stream_tiles(const GemmBatch& batch, uint32_t nb
 #undef QUAD_BODY
 }
 
-// gemm_act_kernels.hip
-hipError_t launch_gemm_act_stream(const GemmBatch& batch, const GemmActArgs& act, int d_bf16, int variant, uint32_t blocks, hipStream_t st);
+// gemm_act_kernels.h
+template <bool OUT_BF16>
+hipError_t launch_gemm_act_stream(const GemmBatch& batch, const GemmActArgs& act, int variant, uint32_t blocks, hipStream_t st);
 
 }  // namespace quartet
