@@ -58,7 +58,7 @@ int quartet_mxfp4_gemm_act(const uint8_t *a_codes, const uint8_t *a_scales, cons
  * dy, pre, multiplier, dz, dmul: bf16 [m x ld], m, n >= 0, leading dimensions multiples of 8 and at least n; dz, dmul and dbias may each be
  * NULL (not all three), multiplier may be NULL (ones); pre may be NULL for QUARTET_ACT_NONE without dmul.  dz may be dy itself, and dmul may be
  * multiplier or pre itself (with the same leading dimension).  workspace: quartet_act_bwd_workspace_bytes(m, n) bytes, 16-byte aligned, needed only
- * with dbias.  m, n < 2^31.
+ * with dbias.  m < 2^31, n <= 2^26.
  */
 size_t quartet_act_bwd_workspace_bytes(int64_t m, int64_t n);
 int quartet_act_bwd(const void *dy_bf16, int64_t lddy, const void *pre_bf16, int64_t ldpre, const void *multiplier_bf16, int64_t ldmul,
@@ -100,7 +100,7 @@ int quartet_rmsnorm_bwd(const void *dy_bf16, int64_t lddy, const void *h, int h_
  * in place, same type): then nothing is written where the factor is 1.  No out may overlap any other out or grad (QUARTET_EINVAL).  A norm that is not
  * finite stands for a step to be skipped: the factor is 1 then, so out holds the gradients as they are.  norm: one device float.  max_norm >= 0; INFINITY: no
  * clipping, and with out = grad just the norm.  The squares are summed in fp64, in an order that depends on the sizes alone.  workspace:
- * quartet_grad_clip_workspace_bytes() bytes, 16-byte aligned.  The sizes together are below 2^43; count <= 2^20.
+ * quartet_grad_clip_workspace_bytes() bytes, 16-byte aligned.  The sizes together are below 2^43; count <= 2^15.
  */
 typedef struct quartet_grad_tensor {
     const void *grad;

@@ -83,7 +83,9 @@ struct ActPlan {
 // One row a wave; with the bias's gradient four: every block leaves a row of partial sums (us, 16 / 32 / 64 / 128 rows a block: 1003 x 5632 10.7 / 11.8 / 17.1 /
 // 29.5, 4096 x 5632 31.8 / 32.8 / 33.8 / 45.9, 16384 x 11008 185 / 186 / 200 / 219, 16384 x 4096 77 / 80 / 85 / 74).
 ActPlan act_plan(int64_t m, int64_t n, bool sums) {
-    const int64_t cb = (n + 511) / 512, rows = sums ? 16 : 4;
+    const int64_t cb = (n + 511) / 512;
+    int64_t rows = sums ? 16 : 4;
+    while ((m + rows - 1) / rows * cb > ((int64_t)1 << 23) && rows < m) rows *= 2;      // a launch has fewer than 2^32 threads
     return {(uint32_t)cb, (uint32_t)((m + rows - 1) / rows), (uint32_t)rows};
 }
 

@@ -17,7 +17,7 @@ using quartet::ProfileScope;
 
 namespace {
 
-constexpr int64_t kMaxNorm = 32768;
+constexpr int64_t kMaxNorm = 32768, kMaxActColumns = (int64_t)1 << 26;
 
 bool is_dtype(int t) { return t == QUARTET_DTYPE_F32 || t == QUARTET_DTYPE_BF16; }
 bool is_activation(int a) { return a >= QUARTET_ACT_NONE && a <= QUARTET_ACT_SILU; }
@@ -78,7 +78,7 @@ int quartet_mxfp4_gemm_act(const uint8_t* a_codes, const uint8_t* a_scales, cons
 }
 
 size_t quartet_act_bwd_workspace_bytes(int64_t m, int64_t n) {
-    if (m < 0 || n < 0 || m >= ((int64_t)1 << 31) || n >= ((int64_t)1 << 31)) return 0;
+    if (m < 0 || n < 0 || m >= ((int64_t)1 << 31) || n > kMaxActColumns) return 0;
     return quartet::act_bwd_workspace(m, n);
 }
 
@@ -95,7 +95,7 @@ int quartet_act_bwd(const void* dy_bf16, int64_t lddy, const void* pre_bf16, int
     if (dz_bf16 && ((dz_bf16 == dy_bf16 && lddz != lddy) || dz_bf16 == dmul_bf16 || dz_bf16 == pre_bf16 || dz_bf16 == multiplier_bf16)) return QUARTET_EINVAL;
     if (dmul_bf16 && (dmul_bf16 == dy_bf16 || (dmul_bf16 == pre_bf16 && lddmul != ldpre) || (dmul_bf16 == multiplier_bf16 && lddmul != ldmul)))
         return QUARTET_EINVAL;
-    if (m >= ((int64_t)1 << 31) || n >= ((int64_t)1 << 31)) return QUARTET_ENOTSUP;
+    if (m >= ((int64_t)1 << 31) || n > kMaxActColumns) return QUARTET_ENOTSUP;
     const size_t need = dbias ? quartet::act_bwd_workspace(m, n) : 0;
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return QUARTET_EINVAL;
     const quartet::ActBwdArgs a = {static_cast<const uint16_t*>(dy_bf16), static_cast<const uint16_t*>(pre_bf16),
@@ -134,7 +134,7 @@ int quartet_rmsnorm_fwd(const void* x, int x_dtype, int64_t ldx, const void* res
     if (h && ((h == residual && ldh != ldres) || (h == x && (x_dtype != h_dtype || ldh != ldx)) || h == y_bf16)) return QUARTET_EINVAL;
     if (y_bf16 && (y_bf16 == x || y_bf16 == residual)) return QUARTET_EINVAL;
     const quartet::NormFwdArgs a = {x, residual, weight, h, y_bf16, codes, scales, mask, rstd, ldx, ldres, ldh, ldy, (uint32_t)rows, (uint32_t)n, eps,
-                                    x_dtype == QUARTET_DTYPE_F32, residual && h_dtype == QUARTET_DTYPE_F32, weight_dtype == QUARTET_DTYPE_F32};
+                                    x_dtype == QUARTET_DTYPE_F32, residual && h_dtype == QUARTET_DTYPE_F32, weight_dtype == QUARTET_DTYPE_F32, false, false, 0.0};
     ProfileScope prof(QUARTET_KIND_NORM, (hipStream_t)stream);
     const hipError_t e = quartet::launch_rmsnorm_fwd(a, format, (hipStream_t)stream);
     return e == hipSuccess ? QUARTET_OK : hip_fail(e);
@@ -177,7 +177,7 @@ int quartet_grad_clip(const quartet_grad_tensor* tensors, int64_t count, float m
     if (count < 0 || (count > 0 && !tensors) || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u)) return QUARTET_EINVAL;
     if (!(max_norm >= 0.0f)) return QUARTET_EINVAL;
     if (!workspace || !aligned16(workspace) || workspace_bytes < quartet::kClipWorkspaceBytes) return QUARTET_EINVAL;
-    if (count > ((int64_t)1 << 20)) return QUARTET_ENOTSUP;
+    if (count > ((int64_t)1 << 15)) return QUARTET_ENOTSUP;       // a sum in the workspace each
     int64_t total = 0;
     for (int64_t i = 0; i < count; ++i) {
         const quartet_grad_tensor& t = tensors[i];

@@ -17,6 +17,8 @@ struct NormFwdArgs {
     uint32_t rows, n;
     float eps;
     bool x_f32, h_f32, w_f32;
+    bool by_tile, past;           // set by the launcher
+    double inv_n;
 };
 struct NormBwdArgs {
     const void *dy, *h, *weight, *dh;
@@ -44,7 +46,8 @@ struct ActBwdArgs {
 size_t act_bwd_workspace(int64_t m, int64_t n);
 hipError_t launch_act_bwd(const ActBwdArgs& a, float* dbias, float* workspace, hipStream_t st);
 
-constexpr size_t kClipWorkspaceBytes = 2048 * sizeof(double);
+constexpr uint32_t kClipPartials = 1u << 16;                                       // sums of squares, then the factor
+constexpr size_t kClipWorkspaceBytes = kClipPartials * sizeof(double) + 16;
 hipError_t launch_grad_clip(const quartet_grad_tensor* tensors, int64_t count, float max_norm, float* norm, double* workspace, hipStream_t st);
 
 // the epilogue of quartet_mxfp4_gemm_act; kinds: 0 = none, 1 = bf16, 2 = fp32

@@ -1,7 +1,8 @@
 // Norm of all gradients of a step and their scaled copies.  Bound by memory: every gradient is read for the norm, which must be known before the
-// first copy is written, and read again for its copy.  The tensors are cut into chunks of kChunk elements; the blocks take chunks b, b + B, ...
-// of all tensors, so a list of many small tensors and one of a few large ones fill the chip alike.  A launch's arguments hold up to kTensors tensors;
-// longer lists take more launches, each adding to the blocks' sums of squares in the workspace (in launch order: the bits do not depend on timing).
+// first copy is written, and read again for its copy.  The tensors are cut into chunks of kChunk elements, a block each: a list of many small tensors and
+// one of a few large ones fill the chip alike, and the blocks in flight cover neighbouring memory.  Every chunk leaves its sum of squares in the workspace (in
+// fixed places and added up in a fixed order: the bits do not depend on timing); where the chunks are few, every block of the second kernel adds them up for itself, otherwise a
+// kernel of one block does.  A launch's arguments hold up to kTensors tensors; longer lists take more launches.
 #include <math.h>
 
 #include "block_common.h"
@@ -11,7 +12,8 @@ namespace quartet {
 
 namespace {
 
-constexpr uint32_t kChunk = 8192, kBlocks = 2048;
+constexpr uint32_t kChunk = 4096;              // (180 small tensors: 36.1 us with 8192, 31.8 with 4096; large ones alike)
+constexpr uint32_t kFew = 1024;                 // chunks that every block adds up for itself
 constexpr int kTensors = 80;
 
 struct ClipTensor {
@@ -55,19 +57,46 @@ __device__ __forceinline__ void load8(const void* p, bool f32, uint64_t at, uint
         if (at + i < size) v[i] = f32 ? static_cast<const float*>(p)[at + i] : bf16_lo(static_cast<const uint16_t*>(p)[at + i]);
     }
 }
-__device__ __forceinline__ void store8(void* p, bool f32, uint64_t at, uint64_t size, bool aligned, const float (&v)[8]) {
-    if (aligned && at + 8u <= size) {
+// Elements at .. at + 3, aligned to their size: what the second kernel goes by.  A store instruction of a wave then writes whole lines, in fp32 too: with eight a
+// lane, two stores of 16 bytes 32 apart, 202 M values from bf16 to fp32 took 352 us in place of 260.
+template <bool PAST>
+__device__ __forceinline__ void load4(const void* p, bool f32, uint64_t at, uint64_t size, bool aligned, float (&v)[4]) {
+    if (aligned && at + 4u <= size) {
         if (f32) {
-            float4* d = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-            d[0] = make_float4(v[0], v[1], v[2], v[3]);
-            d[1] = make_float4(v[4], v[5], v[6], v[7]);
+            const v4f* s = reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at);
+            const v4f t = PAST ? __builtin_nontemporal_load(s) : *s;
+            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
         } else {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = pack8(v);
+            const v2u_t* s = reinterpret_cast<const v2u_t*>(static_cast<const uint16_t*>(p) + at);
+            const v2u_t t = PAST ? __builtin_nontemporal_load(s) : *s;
+            v[0] = bf16_lo(t.x); v[1] = bf16_hi(t.x); v[2] = bf16_lo(t.y); v[3] = bf16_hi(t.y);
         }
         return;
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
+    for (uint32_t i = 0; i < 4; ++i) {
+        v[i] = 0.0f;
+        if (at + i < size) v[i] = f32 ? static_cast<const float*>(p)[at + i] : bf16_lo(static_cast<const uint16_t*>(p)[at + i]);
+    }
+}
+template <bool PAST>
+__device__ __forceinline__ void store4(void* p, bool f32, uint64_t at, uint64_t size, bool aligned, const float (&v)[4]) {
+    if (aligned && at + 4u <= size) {
+        if (f32) {
+            const v4f t = {v[0], v[1], v[2], v[3]};
+            v4f* d = reinterpret_cast<v4f*>(static_cast<float*>(p) + at);
+            if (PAST) __builtin_nontemporal_store(t, d);
+            else *d = t;
+        } else {
+            const v2u_t t = {bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3])};
+            v2u_t* d = reinterpret_cast<v2u_t*>(static_cast<uint16_t*>(p) + at);
+            if (PAST) __builtin_nontemporal_store(t, d);
+            else *d = t;
+        }
+        return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
         if (at + i < size) {
             if (f32) static_cast<float*>(p)[at + i] = v[i];
             else static_cast<uint16_t*>(p)[at + i] = bf16_of(v[i]);
@@ -75,58 +104,88 @@ __device__ __forceinline__ void store8(void* p, bool f32, uint64_t at, uint64_t 
 }
 __device__ __forceinline__ bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0u; }
 
-// sum of a double over the block's 256 threads, in every thread
-__device__ __forceinline__ double block_sum(double s, double* meet) {
+// sum of a double over the block's W waves, in every thread
+template <int W>
+__device__ __forceinline__ double block_sum(double s, double (&meet)[W]) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63u) == 0u) meet[threadIdx.x >> 6] = s;
     __syncthreads();
-    return (meet[0] + meet[1]) + (meet[2] + meet[3]);
+    s = meet[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s += meet[w];
+    return s;
 }
 
+// chunks of kChunk << shift elements
 __global__ void __launch_bounds__(256)
-grad_square_kernel(ClipList l, double* __restrict__ partial, uint32_t add) {
+grad_square_kernel(ClipList l, double* __restrict__ partial, uint32_t shift) {
     __shared__ double meet[4];
+    const ClipTensor& t = tensor_of(l, blockIdx.x);
+    const uint64_t chunk = (uint64_t)kChunk << shift, base = (blockIdx.x - t.first_chunk) * chunk, size = t.size;
+    const bool aligned = is_aligned16(t.grad), f32 = t.grad_f32;
     double s = 0.0;
-    for (uint32_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-        const ClipTensor& t = tensor_of(l, c);
-        const uint64_t base = (uint64_t)(c - t.first_chunk) * kChunk, size = t.size;
-        const bool aligned = is_aligned16(t.grad), f32 = t.grad_f32;
+    for (uint64_t at = base + threadIdx.x * 8u, end = base + chunk < size ? base + chunk : size; at < end; at += kChunk) {
+        float v[kChunk / 2048u][8];
 #pragma unroll
-        for (uint32_t i = 0; i < kChunk / 2048u; ++i) {
-            float v[8];
-            load8(t.grad, f32, base + i * 2048u + threadIdx.x * 8u, size, aligned, v);
+        for (uint32_t i = 0; i < kChunk / 2048u; ++i) load8(t.grad, f32, at + i * 2048u, size, aligned, v[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
-        }
+        for (uint32_t i = 0; i < kChunk / 2048u; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = __builtin_fma((double)v[i][e], (double)v[i][e], s);
     }
     s = block_sum(s, meet);
-    if (threadIdx.x == 0u) partial[blockIdx.x] = add ? partial[blockIdx.x] + s : s;
+    if (threadIdx.x == 0u) partial[blockIdx.x] = s;
 }
 
-__global__ void __launch_bounds__(256)
-grad_scale_kernel(ClipList l, const double* __restrict__ partial, uint32_t partials, float max_norm, float* __restrict__ norm_out) {
-    __shared__ double meet[4];
-    double s = 0.0;
-    for (uint32_t i = threadIdx.x; i < partials; i += 256u) s += partial[i];
-    const float norm = (float)__builtin_sqrt(block_sum(s, meet));
-    if (blockIdx.x == 0u && threadIdx.x == 0u) *norm_out = norm;
+__device__ __forceinline__ float clip_factor(float norm, float max_norm) {
     const float ratio = max_norm / (norm + 1e-6f);
-    const float factor = norm - norm == 0.0f && ratio < 1.0f ? ratio : 1.0f;      // (a norm that is not finite: 1)
-    for (uint32_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-        const ClipTensor& t = tensor_of(l, c);
-        if (t.grad == t.out && factor == 1.0f) continue;
-        const uint64_t base = (uint64_t)(c - t.first_chunk) * kChunk, size = t.size;
-        const bool in = is_aligned16(t.grad), out = is_aligned16(t.out), in32 = t.grad_f32, out32 = t.out_f32;
+    return norm - norm == 0.0f && ratio < 1.0f ? ratio : 1.0f;      // (a norm that is not finite: 1)
+}
+
+__global__ void __launch_bounds__(1024)
+grad_norm_kernel(const double* __restrict__ partial, uint32_t partials, float max_norm, float* __restrict__ norm_out, float* __restrict__ factor_out) {
+    __shared__ double meet[16];
+    double s = 0.0;
+#pragma unroll 8
+    for (uint32_t i = threadIdx.x; i < partials; i += 1024u) s += partial[i];
+    const float norm = (float)__builtin_sqrt(block_sum(s, meet));
+    if (threadIdx.x != 0u) return;
+    *norm_out = norm;
+    *factor_out = clip_factor(norm, max_norm);
+}
+
+// partials: of all chunks, if they are few; otherwise 0, and the factor is known.  The last chunks first: they are what the caches hold of the first pass.
+template <bool PAST>
+__global__ void __launch_bounds__(256)
+grad_scale_kernel(ClipList l, const double* __restrict__ partial, uint32_t partials, float max_norm, float* __restrict__ norm_out,
+                  const float* __restrict__ factor_in, uint32_t shift) {
+    __shared__ double meet[4];
+    float factor;
+    if (partials) {
+        double s = 0.0;
+        for (uint32_t i = threadIdx.x; i < partials; i += 256u) s += partial[i];
+        const float norm = (float)__builtin_sqrt(block_sum(s, meet));
+        if (blockIdx.x == 0u && threadIdx.x == 0u) *norm_out = norm;
+        factor = clip_factor(norm, max_norm);
+    } else {
+        factor = *factor_in;
+    }
+    const uint32_t c = l.chunks - 1u - blockIdx.x;
+    const ClipTensor& t = tensor_of(l, c);
+    if (t.grad == t.out && factor == 1.0f) return;
+    const uint64_t chunk = (uint64_t)kChunk << shift, base = (c - t.first_chunk) * chunk, size = t.size;
+    const bool in32 = t.grad_f32, out32 = t.out_f32;
+    const bool in = (reinterpret_cast<uintptr_t>(t.grad) & (in32 ? 15u : 7u)) == 0u, out = (reinterpret_cast<uintptr_t>(t.out) & (out32 ? 15u : 7u)) == 0u;
+    for (uint64_t at = base + threadIdx.x * 4u, end = base + chunk < size ? base + chunk : size; at < end; at += kChunk) {
+        float v[kChunk / 1024u][4];
 #pragma unroll
-        for (uint32_t i = 0; i < kChunk / 2048u; ++i) {
-            const uint64_t at = base + i * 2048u + threadIdx.x * 8u;
-            if (at >= size) continue;
-            float v[8];
-            load8(t.grad, in32, at, size, in, v);
+        for (uint32_t i = 0; i < kChunk / 1024u; ++i) load4<PAST>(t.grad, in32, at + i * 1024u, size, in, v[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= factor;
-            store8(t.out, out32, at, size, out, v);
+        for (uint32_t i = 0; i < kChunk / 1024u; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] *= factor;
+            store4<PAST>(t.out, out32, at + i * 1024u, size, out, v[i]);
         }
     }
 }
@@ -134,31 +193,40 @@ grad_scale_kernel(ClipList l, const double* __restrict__ partial, uint32_t parti
 }  // namespace
 
 hipError_t launch_grad_clip(const quartet_grad_tensor* tensors, int64_t count, float max_norm, float* norm, double* workspace, hipStream_t st) {
+    uint32_t shift = 0u;
+    uint64_t all = 0u;
+    for (;; ++shift) {            // the smallest chunks whose sums the workspace holds
+        all = 0u;
+        for (int64_t i = 0; i < count; ++i) all += ((uint64_t)tensors[i].size + ((uint64_t)kChunk << shift) - 1u) / ((uint64_t)kChunk << shift);
+        if (all <= kClipPartials || shift >= 40u) break;
+    }
+    if (all > kClipPartials) return hipErrorInvalidValue;
     auto fill = [&](ClipList& l, int64_t& at) {     // the next tensors of the list
         l.count = l.chunks = 0u;
         for (; at < count && l.count < (uint32_t)kTensors; ++at) {
             const quartet_grad_tensor& t = tensors[at];
             if (t.size <= 0) continue;
             l.t[l.count++] = {t.grad, t.out, (uint64_t)t.size, l.chunks, (uint16_t)(t.grad_dtype == QUARTET_DTYPE_F32), (uint16_t)(t.out_dtype == QUARTET_DTYPE_F32)};
-            l.chunks += (uint32_t)(((uint64_t)t.size + kChunk - 1u) / kChunk);
+            l.chunks += (uint32_t)(((uint64_t)t.size + ((uint64_t)kChunk << shift) - 1u) / ((uint64_t)kChunk << shift));
         }
     };
-    uint64_t all = 0;
-    for (int64_t i = 0; i < count; ++i) all += ((uint64_t)tensors[i].size + kChunk - 1u) / kChunk;
-    const uint32_t blocks = all < 1u ? 1u : all < kBlocks ? (uint32_t)all : kBlocks;
+    float* factor = reinterpret_cast<float*>(workspace + kClipPartials);
+    const bool few = all <= kFew;
+    // What the memory-side cache cannot hold goes past it in the second pass (us, through the caches / past them: 202 M values 300 / 260, 51 M fp32 118 / 99).
+    const bool past = all * ((uint64_t)kChunk << shift) >= ((uint64_t)32 << 20);
     ClipList l;
-    int64_t at = 0;
-    uint32_t add = 0u;
-    do {
+    double* partial = workspace;
+    for (int64_t at = 0; at < count; partial += l.chunks) {
         fill(l, at);
-        hipLaunchKernelGGL(grad_square_kernel, dim3(blocks), dim3(256), 0, st, l, workspace, add);
-        add = 1u;
-    } while (at < count);
-    at = 0;
-    do {
+        if (l.chunks) hipLaunchKernelGGL(grad_square_kernel, dim3(l.chunks), dim3(256), 0, st, l, partial, shift);
+    }
+    if (!few || all == 0u) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, workspace, (uint32_t)all, max_norm, norm, factor);
+    for (int64_t at = 0; at < count;) {
         fill(l, at);
-        hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks), dim3(256), 0, st, l, workspace, blocks, max_norm, norm);
-    } while (at < count);
+        if (l.chunks == 0u) continue;
+        if (past) hipLaunchKernelGGL((grad_scale_kernel<true>), dim3(l.chunks), dim3(256), 0, st, l, workspace, few ? (uint32_t)all : 0u, max_norm, norm, factor, shift);
+        else hipLaunchKernelGGL((grad_scale_kernel<false>), dim3(l.chunks), dim3(256), 0, st, l, workspace, few ? (uint32_t)all : 0u, max_norm, norm, factor, shift);
+    }
     return hipGetLastError();
 }
 

@@ -1,4 +1,5 @@
 // Root-mean-square norm of the residual stream, into bf16 or straight into a linear layer's MX operand, and its backward pass.
+// Bound by memory: every value is read once, held in registers across the row's sum, and every result written once.
 #include "block_common.h"
 #include "block_launchers.h"
 
@@ -44,12 +45,16 @@ __device__ __forceinline__ uint4 u4(v4u_t v) { return make_uint4(v.x, v.y, v.z, 
 struct Raw8 {
     uint4 lo, hi;      // bf16: lo
 };
+constexpr int kNonTemporal = 2;      // cache policy of a buffer access
+// PAST: past the caches
+template <bool PAST = false>
 __device__ __forceinline__ void load8(Raw8& r, const Row& row, bool f32, uint32_t col) {
+    constexpr int policy = PAST ? kNonTemporal : 0;
     if (f32) {
-        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u), 0, 0));
-        r.hi = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u + 16u), 0, 0));
+        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u), 0, policy));
+        r.hi = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 4u + 16u), 0, policy));
     } else {
-        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 2u), 0, 0));
+        r.lo = u4(__builtin_amdgcn_raw_buffer_load_b128(row.res, (int)(col * 2u), 0, policy));
     }
 }
 // the lane whose columns are the row's last, incomplete chunk: `left` = 1 .. 7 values (other lanes: 0)
@@ -73,15 +78,17 @@ __device__ __forceinline__ void values8(const Raw8& r, bool f32, float* v) {
         unpack8(r.lo, v);
     }
 }
+template <bool PAST>
 __device__ __forceinline__ void store8(const Row& row, bool f32, uint32_t col, uint32_t tail, const float* v) {
+    constexpr int policy = PAST ? kNonTemporal : 0;
     if (f32) {
         const v4u_t lo = {f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])}, hi = {f2u(v[4]), f2u(v[5]), f2u(v[6]), f2u(v[7])};
-        __builtin_amdgcn_raw_buffer_store_b128(lo, row.res, (int)(col * 4u), 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b128(hi, row.res, (int)(col * 4u + 16u), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(lo, row.res, (int)(col * 4u), 0, policy);
+        __builtin_amdgcn_raw_buffer_store_b128(hi, row.res, (int)(col * 4u + 16u), 0, policy);
     } else {
         const uint4 q = pack8(v);
         const v4u_t d = {q.x, q.y, q.z, q.w};
-        __builtin_amdgcn_raw_buffer_store_b128(d, row.res, (int)(col * 2u), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(d, row.res, (int)(col * 2u), 0, policy);
     }
     if (tail == 0u) return;
 #pragma unroll
@@ -93,6 +100,12 @@ __device__ __forceinline__ void store8(const Row& row, bool f32, uint32_t col, u
 }
 // how many values the lane with columns col .. col + 7 has of the row's incomplete chunk
 __device__ __forceinline__ uint32_t tail_of(uint32_t col, uint32_t n) { return col == (n & ~7u) ? n & 7u : 0u; }
+
+// The scale bytes of a row's 256 columns (one per four lanes, 32 lanes) as the two dwords of its scale tile: lanes 0 and 4 of the 32 hold them afterwards.
+__device__ __forceinline__ uint32_t scale_dword(uint32_t b) {
+    uint32_t w = b | ((uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x108 /* row_shl:8 */, 0xF, 0xF, true) << 8);
+    return w | ((uint32_t)__shfl_down((int)w, 16) << 16);
+}
 
 // Eight columns of one row in each lane; the WPR waves of a row meet in LDS.
 // sum of `part` over the row's lanes, the same bits in all of them
@@ -108,14 +121,53 @@ __device__ __forceinline__ float row_sum(float part, float* meet, uint32_t slot,
     return s;
 }
 
+// Blocks go to the XCDs in turn.  The first row of block b where the 32 rows of a scale tile are to meet in one L2: tiles t, t + 8, ... on XCD t % 8.
+template <uint32_t RPB>
+__device__ __forceinline__ uint32_t tile_row(uint32_t b) {
+    constexpr uint32_t PER = 32u / RPB;                                  // blocks of a tile
+    const uint32_t i = b >> 3;
+    return ((i / PER) * 8u + (b & 7u)) * 32u + (i % PER) * RPB;
+}
+
+// value of lane (l ^ XOR) of a double
+template <int XOR>
+__device__ __forceinline__ double lane_xor64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = f2u(lane_xor<XOR>(u2f((uint32_t)u))), hi = f2u(lane_xor<XOR>(u2f((uint32_t)(u >> 32))));
+    return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+}
+// The sum of squares over the row in 64 bits (the lanes' own eight in 32): what is left of rounding in the statistic is its own last one, and a code that lies
+// next to the middle of two falls as the exact value does about twice as often as with 32 bits.
+template <int WPR>
+__device__ __forceinline__ double row_sum64(double s, double* meet, uint32_t slot, uint32_t sub, uint32_t lane) {
+    s += lane_xor64<1>(s);
+    s += lane_xor64<2>(s);
+    s += lane_xor64<4>(s);
+    s += __shfl_xor(s, 8);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (WPR == 1) return s;
+    if (lane == 0) meet[slot * WPR + sub] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) s += meet[slot * WPR + w];
+    return s;
+}
+// 1 / sqrt(x) from the hardware's 64-bit estimate and one Newton step, rounded once (0, infinities and NaN as the estimate has them)
+__device__ __forceinline__ float rsqrt_once(double x) {
+    const double r = __builtin_amdgcn_rsq(x), better = r * (1.5 - 0.5 * x * r * r);
+    return (float)(better == better ? better : r);
+}
+
 // A row belongs to WPR waves; lane l of wave `sub` of a row holds the columns 8 ((j WPR + sub) 64 + l) .. + 7 of chunk j < CH.
 template <int WPR, int CH, int FMT>
 __global__ void __launch_bounds__(WPR < 4 ? 256 : 64 * WPR)
 rmsnorm_fwd_kernel(NormFwdArgs a) {
     constexpr uint32_t THREADS = WPR < 4 ? 256 : 64 * WPR, RPB = THREADS / 64 / WPR;
-    __shared__ float meet[THREADS / 64];
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t slot = wave / WPR, sub = wave % WPR, row = blockIdx.x * RPB + slot;
+    __shared__ double meet[THREADS / 64];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = blockIdx.y * gridDim.x + blockIdx.x;
+    const uint32_t slot = wave / WPR, sub = wave % WPR, row = a.by_tile ? tile_row<RPB>(block) + slot : block * RPB + slot;
     const bool in = row < a.rows;
     const uint32_t n = a.n;
     const uint32_t n_in = in ? n : 0u;
@@ -146,7 +198,7 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
         }
     }
     float v[CH][8];
-    float part = 0.0f;
+    double part = 0.0;
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
         values8(rx[j], a.x_f32, v[j]);
@@ -159,15 +211,14 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
                 const uint4 q = pack8(v[j]);
                 unpack8(q, v[j]);
             }
-            if (a.h) store8(h_row, a.h_f32, col[j], tail[j], v[j]);
+            if (a.h) store8<true>(h_row, a.h_f32, col[j], tail[j], v[j]);
         }
         float t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = v[j][i] * v[j][i];
-        part += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        part += (double)(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     }
-    const float ss = row_sum<WPR>(part, meet, slot, sub, lane);
-    const float rstd = 1.0f / __builtin_sqrtf(ss / (float)n + a.eps);
+    const float rstd = rsqrt_once(row_sum64<WPR>(part, meet, slot, sub, lane) * a.inv_n + (double)a.eps);
     if (a.rstd && in && sub == 0u && lane == 0u) a.rstd[row] = rstd;
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
@@ -175,11 +226,25 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
         values8(rw[j], a.w_f32, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * rstd * w[i];
-        if (a.y) store8(y_row, false, col[j], tail[j], v[j]);
+        if (a.y) {
+            if (a.past) store8<true>(y_row, false, col[j], tail[j], v[j]);
+            else store8<false>(y_row, false, col[j], tail[j], v[j]);
+        }
         if (FMT == kFmtNone) continue;
         // a group is four consecutive lanes; n is a multiple of 32, so it exists as a whole or not at all
         const bool there = in && col[j] < n;
-        const uint32_t g = col[j] >> 5, kqs = (n + 255u) >> 8;
+        const uint32_t g = col[j] >> 5, kqs = (n + 255u) >> 8, at32 = lane & 31u;
+        auto store_scale = [&](uint32_t b) __attribute__((always_inline)) {
+            const uint32_t w = scale_dword(b), h = at32 >> 2;            // lanes 0 and 4: groups h, 2 + h, 4 + h, 6 + h of the K-quad
+            if (!there || (at32 != 0u && at32 != 4u)) return;
+            uint8_t* dst = a.scales + scale_tile_offset(row, g, kqs);
+            if ((n & 255u) == 0u || (col[j] | 255u) < n) {
+                *reinterpret_cast<uint32_t*>(dst) = w;
+            } else {                                                     // a ragged last K-quad: bytes of groups past n are not written
+                for (uint32_t i = 0; i < 4u; ++i)
+                    if ((g & ~7u) + 2u * i + h < (n >> 5)) dst[i] = (uint8_t)(w >> (8u * i));
+            }
+        };
         if (FMT == kFmtMx8) {
             float mx = 0.0f;
 #pragma unroll
@@ -192,9 +257,12 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[i] = __builtin_amdgcn_fmed3f(v[j][i] * mult, -448.0f, 448.0f);
             if (there) {
-                *reinterpret_cast<uint2*>(a.codes + (size_t)row * n + col[j]) = make_uint2(e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7]));
-                if ((lane & 3u) == 0u) a.scales[scale_tile_offset(row, g, kqs)] = (uint8_t)b;
+                const v2u_t c = {e4m3x4(q[0], q[1], q[2], q[3]), e4m3x4(q[4], q[5], q[6], q[7])};
+                v2u_t* dst = reinterpret_cast<v2u_t*>(a.codes + (size_t)row * n + col[j]);
+                if (a.past) __builtin_nontemporal_store(c, dst);
+                else *dst = c;
             }
+            store_scale(b);
         } else {
             // 32-point transform: strides 1, 2, 4 in the lane, 8 and 16 between lanes (own * t + partner: a + b below, a - b above)
 #pragma unroll
@@ -230,21 +298,24 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
             m |= f2u(lane_xor<1>(u2f(m)));
             m |= f2u(lane_xor<2>(u2f(m)));
             if (there) {
-                *reinterpret_cast<uint32_t*>(a.codes + (size_t)row * (n >> 1) + (col[j] >> 1)) = e2m1x8(v[j], scale);
-                if ((lane & 3u) == 0u) {
-                    a.scales[scale_tile_offset(row, g, kqs)] = (uint8_t)b;
-                    if (a.mask) a.mask[(size_t)row * (n >> 5) + g] = m;
-                }
+                uint32_t* dst = reinterpret_cast<uint32_t*>(a.codes + (size_t)row * (n >> 1) + (col[j] >> 1));
+                if (a.past) store_stream4(dst, e2m1x8(v[j], scale));
+                else *dst = e2m1x8(v[j], scale);
+                if (a.mask && (lane & 3u) == 0u) a.mask[(size_t)row * (n >> 5) + g] = m;
             }
+            store_scale(b);
         }
     }
 }
 
 // Backward: a block goes through the rows blockIdx.x RPB + slot, + gridDim.x RPB, ...; the weight and its gradient's partial sums stay in
 // registers, the latter meet in LDS and go to the workspace, one row of n floats per block.
-template <int WPR, int CH>
+// With the next row's loads ahead of the reduction, against one row at a time (us): 16384 x 4096 bf16 111 -> 94, 4096 x 8192 57 -> 40, 8192 x 2048 fp32 59 -> 56.
+// PAST: more is read than the memory-side cache holds.
+template <int WPR, int CH, bool PAST>
 __global__ void __launch_bounds__(WPR < 4 ? 256 : 64 * WPR)
 rmsnorm_bwd_kernel(NormBwdArgs a) {
+    constexpr bool AHEAD = WPR < 16 || CH == 1;      // (the wide rows' 1024 threads have no registers for two rows)
     constexpr uint32_t THREADS = WPR < 4 ? 256 : 64 * WPR, RPB = THREADS / 64 / WPR;
     __shared__ float meet[2][THREADS / 64];
     __shared__ float4 join[RPB > 1 ? THREADS * 2 : 1];
@@ -263,22 +334,22 @@ rmsnorm_bwd_kernel(NormBwdArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
     }
-    uint32_t turn = 0u;
-    for (uint32_t row0 = blockIdx.x * RPB; row0 < a.rows; row0 += gridDim.x * RPB, turn ^= 1u) {     // the same trips for every wave: they meet
-        const uint32_t row = row0 + slot;
+    // the next row's values are on their way while this one's sum is formed and its results leave
+    Raw8 rdy[CH], rh[CH], rd[CH];
+    float rstd = 0.0f;
+    auto load_row = [&](uint32_t row) __attribute__((always_inline)) {
         const bool in = row < a.rows;
         const uint32_t n_in = in ? n : 0u;
         const Row dy_row = row_of(a.dy, false, (size_t)row * a.lddy, n_in), h_row = row_of(a.h, a.h_f32, (size_t)row * a.ldh, n_in);
         const Row dh_row = row_of(a.dh, a.h_f32, (size_t)row * a.lddh, a.dh ? n_in : 0u);
-        Raw8 rdy[CH], rh[CH], rd[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            load8(rdy[j], dy_row, false, col[j]);
-            load8(rh[j], h_row, a.h_f32, col[j]);
+            load8<PAST>(rdy[j], dy_row, false, col[j]);
+            load8<PAST>(rh[j], h_row, a.h_f32, col[j]);
         }
         if (a.dh) {
 #pragma unroll
-            for (int j = 0; j < CH; ++j) load8(rd[j], dh_row, a.h_f32, col[j]);
+            for (int j = 0; j < CH; ++j) load8<PAST>(rd[j], dh_row, a.h_f32, col[j]);
         }
         if ((n & 7u) != 0u) {
 #pragma unroll
@@ -289,40 +360,48 @@ rmsnorm_bwd_kernel(NormBwdArgs a) {
                 if (a.dh) load_tail(rd[j], dh_row, a.h_f32, tail);
             }
         }
-        const float r = in ? a.rstd[row] : 0.0f;
+        rstd = in ? a.rstd[row] : 0.0f;
+    };
+    uint32_t turn = 0u;
+    if (AHEAD) load_row(blockIdx.x * RPB + slot);
+    for (uint32_t row0 = blockIdx.x * RPB; row0 < a.rows; row0 += gridDim.x * RPB, turn ^= 1u) {     // the same trips for every wave: they meet
+        const uint32_t row = row0 + slot;
+        const bool in = row < a.rows;
+        const uint32_t n_in = in ? n : 0u;
+        if (!AHEAD) load_row(row);
+        const float r = rstd;
+        float dy[CH][8], h[CH][8], add[CH][8];
         float part = 0.0f;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            float dy[8], h[8];
-            values8(rdy[j], false, dy);
-            values8(rh[j], a.h_f32, h);
+            values8(rdy[j], false, dy[j]);
+            values8(rh[j], a.h_f32, h[j]);
+            if (a.dh) values8(rd[j], a.h_f32, add[j]);
             float t[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                t[i] = dy[i] * w[j][i] * h[i];
-                dw[j][i] = __builtin_fmaf(dy[i] * r, h[i], dw[j][i]);
+                dw[j][i] = __builtin_fmaf(dy[j][i] * r, h[j][i], dw[j][i]);
+                dy[j][i] *= w[j][i];
+                t[i] = dy[j][i] * h[j][i];
             }
             part += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
         }
+        if (AHEAD) load_row(row + gridDim.x * RPB);
         const float c = row_sum<WPR>(part, meet[turn], slot, sub, lane) / (float)n * r * r;
         if (a.dx) {
             const Row dx_row = row_of(a.dx, a.h_f32, (size_t)row * a.lddx, n_in), dx16_row = row_of(a.dx16, false, (size_t)row * a.lddx16, a.dx16 ? n_in : 0u);
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const uint32_t tail = in ? tail_of(col[j], n) : 0u;
-                float dy[8], h[8], d[8];
-                values8(rdy[j], false, dy);
-                values8(rh[j], a.h_f32, h);
+                float d[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = r * (dy[i] * w[j][i] - h[i] * c);
+                for (int i = 0; i < 8; ++i) d[i] = r * (dy[j][i] - h[j][i] * c);
                 if (a.dh) {
-                    float s[8];
-                    values8(rd[j], a.h_f32, s);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] += s[i];
+                    for (int i = 0; i < 8; ++i) d[i] += add[j][i];
                 }
-                store8(dx_row, a.h_f32, col[j], tail, d);
-                if (a.dx16) store8(dx16_row, false, col[j], tail, d);
+                store8<PAST>(dx_row, a.h_f32, col[j], tail, d);
+                if (a.dx16) store8<PAST>(dx16_row, false, col[j], tail, d);
             }
         }
     }
@@ -346,7 +425,7 @@ rmsnorm_bwd_kernel(NormBwdArgs a) {
                 }
             }
         }
-        if (slot == 0u) store8(p_row, true, col[j], 0u, dw[j]);
+        if (slot == 0u) store8<false>(p_row, true, col[j], 0u, dw[j]);
     }
 }
 
@@ -382,44 +461,52 @@ hipError_t launch_column_sum(const float* partial, uint32_t rows, uint32_t pitch
 
 namespace {
 
-// Waves per row and chunks per lane: as few waves as hold a row in four chunks, and more while the rows alone do not give the chip eight waves per
-// compute unit.
+// Waves per row and chunks per lane: a chunk each up to sixteen waves (8192 columns), then more chunks.  Many waves with little each hide the loads of one another
+// and of the reductions (us, four chunks a lane / two / one, forward: 16384 x 4096 into MXFP8 90 / 81 / 79, into bf16 98 / 93 / 88, 2336 x 1376 into MXFP8 9.8 /
+// 8.1 / 7.8; 4096 x 2048 18.1 / 16.0 / 16.0).
 struct NormShape {
     int wpr, ch;
 };
-NormShape norm_shape(int64_t rows, int64_t n, int most_ch) {
+NormShape norm_shape(int64_t n) {
     const int64_t units = (n + 511) / 512;
-    int wpr = 1;
-    while (wpr < 16 && (int64_t)wpr * most_ch < units) wpr *= 2;
-    while (wpr < 16 && wpr < units && rows * wpr < 2048) wpr *= 2;
-    int ch = 1;
+    int wpr = 1, ch = 1;
+    while (wpr < 16 && wpr < units) wpr *= 2;
     while ((int64_t)wpr * ch < units) ch *= 2;
     return {wpr, ch};
 }
 uint32_t rows_per_block(int wpr) { return wpr < 4 ? 4u / (uint32_t)wpr : 1u; }
 
 template <int WPR, int CH>
-void launch_fwd(const NormFwdArgs& a, int format, hipStream_t st) {
-    const dim3 grid((a.rows + rows_per_block(WPR) - 1u) / rows_per_block(WPR)), block(WPR < 4 ? 256 : 64 * WPR);
+void launch_fwd(NormFwdArgs a, int format, hipStream_t st) {
+    const uint32_t rpb = rows_per_block(WPR), tiles = (a.rows + 31u) / 32u;
+    a.by_tile = format != kFmtNone && a.rows >= 1024u;
+    // results that the next kernel reads (bytes) go past the memory-side cache where it cannot hold them, codes as those of the quantizers
+    const double values = (double)a.rows * a.n;
+    a.past = format == kFmtNone ? values * 2.0 >= 256.0 * 1024.0 * 1024.0 : values * (format == kFmtMx8 ? 1.0 : 0.5) >= 64.0 * 1024.0 * 1024.0;
+    a.inv_n = 1.0 / a.n;
+    const uint32_t blocks = a.by_tile ? (tiles + 7u) / 8u * 8u * (32u / rpb) : (a.rows + rpb - 1u) / rpb, wide = blocks < (1u << 20) ? blocks : 1u << 20;
+    const dim3 grid(wide, (blocks + wide - 1u) / wide), block(WPR < 4 ? 256 : 64 * WPR);      // (a dimension has fewer than 2^32 threads)
     if (format == kFmtMx4) hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtMx4>), grid, block, 0, st, a);
     else if (format == kFmtMx8) hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtMx8>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((rmsnorm_fwd_kernel<WPR, CH, kFmtNone>), grid, block, 0, st, a);
 }
 
-constexpr uint32_t kNormBlocks = 1024;      // blocks of a backward pass: partial sums of the weight's gradient
+// Blocks of a backward pass, each a row of partial sums of the weight's gradient.  Two waves per SIMD unit are enough with the next row's loads ahead (us, 256 / 512 /
+// 1024 / 2048 blocks of four waves: 8192 x 2048 fp32 55.1 / 56.0 / 58.6 / 61.8, 2048 x 2048 bf16 12.4 / 11.3 / 12.0 / 15.9; a compute unit each for wider ones:
+// 4096 x 8192 40.4 with 256 blocks of sixteen waves, 57.9 with 128).
 uint32_t bwd_blocks(int64_t rows, int64_t n) {
-    const uint32_t rpb = rows_per_block(norm_shape(rows, n, 2).wpr);
-    const int64_t all = (rows + rpb - 1) / rpb;
-    return (uint32_t)(all < kNormBlocks ? all : kNormBlocks);
+    const int wpr = norm_shape(n).wpr;
+    const int64_t all = (rows + rows_per_block(wpr) - 1) / rows_per_block(wpr), most = wpr <= 4 ? 512 : 256;
+    return (uint32_t)(all < most ? all : most);
 }
 
 }  // namespace
 
-#define NORM_SHAPES(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(2, 4) X(4, 1) X(4, 2) X(4, 4) X(8, 1) X(8, 2) X(8, 4) X(16, 1) X(16, 2) X(16, 4)
+#define NORM_SHAPES(X) X(1, 1) X(2, 1) X(4, 1) X(8, 1) X(16, 1) X(16, 2) X(16, 4)
 
 hipError_t launch_rmsnorm_fwd(const NormFwdArgs& a, int format, hipStream_t st) {
     if (a.rows == 0) return hipSuccess;
-    const NormShape s = norm_shape(a.rows, a.n, 4);
+    const NormShape s = norm_shape(a.n);
 #define NORM_CASE(W, C) if (s.wpr == W && s.ch == C) launch_fwd<W, C>(a, format, st);
     NORM_SHAPES(NORM_CASE)
 #undef NORM_CASE
@@ -435,10 +522,16 @@ hipError_t launch_rmsnorm_bwd(const NormBwdArgs& args, float* dweight, float* wo
     }
     NormBwdArgs a = args;
     a.partial = dweight ? workspace : nullptr;
-    const NormShape s = norm_shape(a.rows, a.n, 2);
+    const NormShape s = norm_shape(a.n);
     const uint32_t blocks = bwd_blocks(a.rows, a.n);
-#define NORM_CASE(W, C) \
-    if (s.wpr == W && s.ch == C) hipLaunchKernelGGL((rmsnorm_bwd_kernel<W, C>), dim3(blocks), dim3(W < 4 ? 256 : 64 * W), 0, st, a);
+    // Where the memory-side cache cannot hold what is read, loads and results go past it: 16384 x 4096 bf16 (402 MB read) 94 -> 88 us; below, the results wait
+    // in it for the layer that takes them (8192 x 2048 fp32, 168 MB read: 56.0 us with results past it, 53.9 without).
+    const bool past = (double)a.rows * a.n * (2.0 + (a.h_f32 ? 4.0 : 2.0) * (a.dh ? 2.0 : 1.0)) >= 256.0 * 1024.0 * 1024.0;
+#define NORM_CASE(W, C)                                                                                                                     \
+    if (s.wpr == W && s.ch == C) {                                                                                                          \
+        if (past) hipLaunchKernelGGL((rmsnorm_bwd_kernel<W, C, true>), dim3(blocks), dim3(W < 4 ? 256 : 64 * W), 0, st, a);                  \
+        else hipLaunchKernelGGL((rmsnorm_bwd_kernel<W, C, false>), dim3(blocks), dim3(W < 4 ? 256 : 64 * W), 0, st, a);                      \
+    }
     NORM_SHAPES(NORM_CASE)
 #undef NORM_CASE
     const hipError_t e = hipGetLastError();

@@ -81,13 +81,14 @@ def test_act_bwd_refuses(b, change):
 
 def test_act_bwd_sizes(b):
     assert b.quartet_act_bwd(**{**ACT, "m": 2 ** 31}) == b.QUARTET_ENOTSUP
+    assert b.quartet_act_bwd(**{**ACT, "n": 2 ** 26 + 8, **{k: 2 ** 26 + 8 for k in ACT if k.startswith("ld")}}) == b.QUARTET_ENOTSUP
     assert b.quartet_act_bwd(**{**ACT, "m": 0, "dbias": None, "workspace": None, "workspace_bytes": 0}) == b.QUARTET_OK
     assert b.quartet_act_bwd(**{**ACT, "n": 0, "workspace": None}) == b.QUARTET_OK
     assert b.quartet_act_bwd_workspace_bytes(4, 20) == 96 and b.quartet_act_bwd_workspace_bytes(0, 20) == 0
     assert b.quartet_act_bwd_workspace_bytes(-1, 20) == 0 and b.quartet_act_bwd_workspace_bytes(2 ** 31, 20) == 0
     for m in (1, 15, 16, 17, 1003, 16384, 2 ** 22, 2 ** 31 - 1):
         for n in (1, 511, 512, 513, 11008, 2 ** 20):
-            assert 0 < b.quartet_act_bwd_workspace_bytes(m, n) <= (2048 / ((n + 511) // 512) + 2) * (n + 7) * 4
+            assert 0 < b.quartet_act_bwd_workspace_bytes(m, n) <= (m + 15) // 16 * (n + 7) * 4
 
 
 NORM = dict(x=P, x_dtype=1, ldx=64, residual=2 * P, ldres=64, rows=4, n=64, weight=3 * P, weight_dtype=0, eps=1e-5, h=4 * P, h_dtype=0, ldh=64, y_bf16=5 * P,

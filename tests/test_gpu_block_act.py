@@ -130,7 +130,8 @@ def check_clip(grads, outs, max_norm, before=None):
     return norm
 
 
-SIZES = [[1], [7, 0, 8, 1], [8192], [8193, 8191, 1], [100000, 3, 77777], [5] * 79, [5] * 80, [33] * 81, [17] * 500, [3000000, 11]]
+SIZES = [[1], [7, 0, 8, 1], [8192], [8193, 8191, 1], [100000, 3, 77777], [5] * 79, [5] * 80, [33] * 81, [17] * 500, [3000000, 11],
+         [4096 * 1024], [4096 * 1024, 1], [9000000, 5, 4097], [34000000, 9]]
 
 
 @pytest.mark.parametrize("g_dtype,o_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
