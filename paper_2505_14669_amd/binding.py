@@ -162,7 +162,7 @@ def quartet_sr_bits():
     return _lib.quartet_sr_bits()
 
 
-KIND_NAMES = ["quant_fwd", "quant_bwd", "requant", "gemm", "epilogue", "dequant", "fp8_quant", "fp8_gemm"]
+KIND_NAMES = ["quant_fwd", "quant_bwd", "requant", "gemm", "epilogue", "dequant", "fp8_quant", "fp8_gemm", "norm", "act", "clip"]
 QUARTET_KIND_GEMM = 3
 
 

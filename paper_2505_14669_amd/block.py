@@ -46,21 +46,15 @@ _lib.quartet_grad_clip_workspace_bytes.argtypes = []
 _lib.quartet_grad_clip.argtypes = [_p, _i64, _f, _p, _p, _size, _p]
 
 
-def _call(name, *args):
-    """through the torch node where that takes the arguments (binding.py says why), else through ctypes"""
-    if _q._native is not None:
-        rc = getattr(_q._native, name)(*args)
-        if rc is not NotImplemented:
-            return rc
-    return None
-
+# Calls go through the torch node where that takes the arguments (binding.py says why), else through ctypes.
 
 def quartet_mxfp4_gemm_act(a_codes, a_scales, b_codes, b_scales, m, n, k, alpha, bias, bias_dtype, activation, multiplier_bf16, ldmul, residual,
                            residual_dtype, ldres, pre_bf16, ldpre, d, d_dtype, ldd, stream=None):
-    rc = _call("quartet_mxfp4_gemm_act", a_codes, a_scales, b_codes, b_scales, m, n, k, alpha, bias, bias_dtype, activation, multiplier_bf16, ldmul,
-               residual, residual_dtype, ldres, pre_bf16, ldpre, d, d_dtype, ldd, stream)
-    if rc is not None:
-        return rc
+    if _q._native is not None:
+        rc = _q._native.quartet_mxfp4_gemm_act(a_codes, a_scales, b_codes, b_scales, m, n, k, alpha, bias, bias_dtype, activation, multiplier_bf16,
+                                               ldmul, residual, residual_dtype, ldres, pre_bf16, ldpre, d, d_dtype, ldd, stream)
+        if rc is not NotImplemented:
+            return rc
     return _lib.quartet_mxfp4_gemm_act(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, alpha, _ptr(bias), bias_dtype,
                                        activation, _ptr(multiplier_bf16), ldmul, _ptr(residual), residual_dtype, ldres, _ptr(pre_bf16), ldpre,
                                        _ptr(d), d_dtype, ldd, _stream(stream))
@@ -72,20 +66,22 @@ def quartet_act_bwd_workspace_bytes(m, n):
 
 def quartet_act_bwd(dy_bf16, lddy, pre_bf16, ldpre, multiplier_bf16, ldmul, m, n, activation, dz_bf16, lddz, dmul_bf16, lddmul, dbias, workspace,
                     workspace_bytes, stream=None):
-    rc = _call("quartet_act_bwd", dy_bf16, lddy, pre_bf16, ldpre, multiplier_bf16, ldmul, m, n, activation, dz_bf16, lddz, dmul_bf16, lddmul, dbias,
-               workspace, workspace_bytes, stream)
-    if rc is not None:
-        return rc
+    if _q._native is not None:
+        rc = _q._native.quartet_act_bwd(dy_bf16, lddy, pre_bf16, ldpre, multiplier_bf16, ldmul, m, n, activation, dz_bf16, lddz, dmul_bf16, lddmul,
+                                        dbias, workspace, workspace_bytes, stream)
+        if rc is not NotImplemented:
+            return rc
     return _lib.quartet_act_bwd(_ptr(dy_bf16), lddy, _ptr(pre_bf16), ldpre, _ptr(multiplier_bf16), ldmul, m, n, activation, _ptr(dz_bf16), lddz,
                                 _ptr(dmul_bf16), lddmul, _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream))
 
 
 def quartet_rmsnorm_fwd(x, x_dtype, ldx, residual, ldres, rows, n, weight, weight_dtype, eps, h, h_dtype, ldh, y_bf16, ldy, format, codes, scales, mask,
                         rstd, stream=None):
-    rc = _call("quartet_rmsnorm_fwd", x, x_dtype, ldx, residual, ldres, rows, n, weight, weight_dtype, eps, h, h_dtype, ldh, y_bf16, ldy, format, codes,
-               scales, mask, rstd, stream)
-    if rc is not None:
-        return rc
+    if _q._native is not None:
+        rc = _q._native.quartet_rmsnorm_fwd(x, x_dtype, ldx, residual, ldres, rows, n, weight, weight_dtype, eps, h, h_dtype, ldh, y_bf16, ldy,
+                                            format, codes, scales, mask, rstd, stream)
+        if rc is not NotImplemented:
+            return rc
     return _lib.quartet_rmsnorm_fwd(_ptr(x), x_dtype, ldx, _ptr(residual), ldres, rows, n, _ptr(weight), weight_dtype, eps, _ptr(h), h_dtype, ldh,
                                     _ptr(y_bf16), ldy, format, _ptr(codes), _ptr(scales), _ptr(mask), _ptr(rstd), _stream(stream))
 
@@ -96,10 +92,11 @@ def quartet_rmsnorm_bwd_workspace_bytes(rows, n):
 
 def quartet_rmsnorm_bwd(dy_bf16, lddy, h, h_dtype, ldh, rows, n, weight, weight_dtype, rstd, dh, lddh, dx, lddx, dx16, lddx16, dweight, workspace,
                         workspace_bytes, stream=None):
-    rc = _call("quartet_rmsnorm_bwd", dy_bf16, lddy, h, h_dtype, ldh, rows, n, weight, weight_dtype, rstd, dh, lddh, dx, lddx, dx16, lddx16, dweight,
-               workspace, workspace_bytes, stream)
-    if rc is not None:
-        return rc
+    if _q._native is not None:
+        rc = _q._native.quartet_rmsnorm_bwd(dy_bf16, lddy, h, h_dtype, ldh, rows, n, weight, weight_dtype, rstd, dh, lddh, dx, lddx, dx16, lddx16,
+                                            dweight, workspace, workspace_bytes, stream)
+        if rc is not NotImplemented:
+            return rc
     return _lib.quartet_rmsnorm_bwd(_ptr(dy_bf16), lddy, _ptr(h), h_dtype, ldh, rows, n, _ptr(weight), weight_dtype, _ptr(rstd), _ptr(dh), lddh,
                                     _ptr(dx), lddx, _ptr(dx16), lddx16, _ptr(dweight), _ptr(workspace), workspace_bytes, _stream(stream))
 
@@ -141,9 +138,10 @@ def quartet_grad_clip_workspace_bytes():
 
 def quartet_grad_clip(tensors, count, max_norm, norm, workspace, workspace_bytes, stream=None):
     address = tensors.address if isinstance(tensors, GradTensors) else tensors
-    rc = _call("quartet_grad_clip", address, count, max_norm, norm, workspace, workspace_bytes, stream)
-    if rc is not None:
-        return rc
+    if _q._native is not None:
+        rc = _q._native.quartet_grad_clip(address, count, max_norm, norm, workspace, workspace_bytes, stream)
+        if rc is not NotImplemented:
+            return rc
     return _lib.quartet_grad_clip(address, count, max_norm, _ptr(norm), _ptr(workspace), workspace_bytes, _stream(stream))
 
 

@@ -87,4 +87,22 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
+// value of lane (l ^ XOR) of a double
+template <int XOR>
+__device__ __forceinline__ double lane_xor64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = f2u(lane_xor<XOR>(u2f((uint32_t)u))), hi = f2u(lane_xor<XOR>(u2f((uint32_t)(u >> 32))));
+    return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+}
+// wave_sum of a double
+__device__ __forceinline__ double wave_sum64(double s) {
+    s += lane_xor64<1>(s);
+    s += lane_xor64<2>(s);
+    s += lane_xor64<4>(s);
+    s += __shfl_xor(s, 8);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    return s;
+}
+
 }  // namespace quartet

@@ -29,14 +29,13 @@ struct ClipList {
 };
 static_assert(sizeof(ClipList) + 64 <= 4096, "a launch's arguments");
 
+// The tensor of a chunk: the last one whose first chunk is not behind it.  Every lane looks at one or two, one trip to memory (a search would wait for several).
 __device__ __forceinline__ const ClipTensor& tensor_of(const ClipList& l, uint32_t chunk) {
-    uint32_t lo = 0u, hi = l.count;            // the last tensor whose first chunk is not behind this one
-    while (hi - lo > 1u) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (l.t[mid].first_chunk <= chunk) lo = mid;
-        else hi = mid;
-    }
-    return l.t[lo];
+    static_assert(kTensors > 64 && kTensors <= 128, "two tensors a lane");
+    const uint32_t lane = threadIdx.x & 63u, high = lane + 64u;
+    const bool a = lane < l.count && l.t[lane].first_chunk <= chunk, b = high < l.count && l.t[high < (uint32_t)kTensors ? high : 0u].first_chunk <= chunk;
+    const int before = __popcll(__ballot(a)) + __popcll(__ballot(b));
+    return l.t[__builtin_amdgcn_readfirstlane(before) - 1];
 }
 
 // elements at .. at + 7 of a tensor of `size` (missing ones: 0); whole: eight of them, aligned to 16 bytes
@@ -107,8 +106,7 @@ __device__ __forceinline__ bool is_aligned16(const void* p) { return (reinterpre
 // sum of a double over the block's W waves, in every thread
 template <int W>
 __device__ __forceinline__ double block_sum(double s, double (&meet)[W]) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
+    s = wave_sum64(s);
     if ((threadIdx.x & 63u) == 0u) meet[threadIdx.x >> 6] = s;
     __syncthreads();
     s = meet[0];

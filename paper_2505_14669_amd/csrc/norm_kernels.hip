@@ -129,23 +129,11 @@ __device__ __forceinline__ uint32_t tile_row(uint32_t b) {
     return ((i / PER) * 8u + (b & 7u)) * 32u + (i % PER) * RPB;
 }
 
-// value of lane (l ^ XOR) of a double
-template <int XOR>
-__device__ __forceinline__ double lane_xor64(double x) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = f2u(lane_xor<XOR>(u2f((uint32_t)u))), hi = f2u(lane_xor<XOR>(u2f((uint32_t)(u >> 32))));
-    return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
-}
 // The sum of squares over the row in 64 bits (the lanes' own eight in 32): what is left of rounding in the statistic is its own last one, and a code that lies
 // next to the middle of two falls as the exact value does about twice as often as with 32 bits.
 template <int WPR>
 __device__ __forceinline__ double row_sum64(double s, double* meet, uint32_t slot, uint32_t sub, uint32_t lane) {
-    s += lane_xor64<1>(s);
-    s += lane_xor64<2>(s);
-    s += lane_xor64<4>(s);
-    s += __shfl_xor(s, 8);
-    s += __shfl_xor(s, 16);
-    s += __shfl_xor(s, 32);
+    s = wave_sum64(s);
     if (WPR == 1) return s;
     if (lane == 0) meet[slot * WPR + sub] = s;
     __syncthreads();

@@ -91,6 +91,25 @@ def test_in_place(m, n, k):
     assert torch.equal(product(rng(8), m, n, k, res=BF16, out=BF16, in_place="res"), want)
 
 
+def test_rows_far_apart():
+    # rows of 2^21 elements: the last ones lie past 2^32 bytes, in the split kernels and in the streaming ones
+    m, n, k, ld = 1100, 64, 64, 2 ** 21
+    A, As, a = quantized(rng(17), m, k)
+    B, Bs, w = quantized(rng(18), n, k, 0.1)
+    res, d = torch.empty((m, ld), device=DEV), torch.empty((m, ld), dtype=BF16, device=DEV)
+    res[:, :n] = torch.randn((m, n), generator=rng(19), device=DEV)
+    want = a @ w.t() + res[:, :n].double()
+    off = 5 * 2.0 ** -23 * (a.abs() @ w.abs().t() + res[:, :n].double().abs()) + want.abs() * U16 * 1.01
+    try:
+        for variant in (-1, 0, 1, 2, 22):
+            q.check(q.quartet_debug_set_gemm_plan(variant, 0))
+            d[:, :n] = GUARD
+            q.check(b.quartet_mxfp4_gemm_act(A, As, B, Bs, m, n, k, 1.0, None, 0, 0, None, 0, res, 0, ld, None, 0, d, 1, ld))
+            assert_within(d[:, :n], want, off, variant)
+    finally:
+        q.quartet_debug_set_gemm_plan(-1, 0)
+
+
 # every kernel that the sizes pick: block tiles of 256 x 256, 128 x 256, 128 x 128 (one block and two per compute unit) and the in-block split's
 @pytest.mark.parametrize("m,n,k", [(4096, 4096, 1024), (2100, 4448, 320), (4096, 2048, 2048), (2048, 2048, 4096), (10327, 992, 800), (1003, 5632, 2048), (16640, 1280, 256)])
 @pytest.mark.parametrize("epilogue", [dict(kind="gelu", bias=BF16, pre=True), dict(kind="silu", mul=True), dict(res=F32, out=F32), dict(res=BF16), FULL], ids=str)
