@@ -46,7 +46,7 @@ struct ActBwdArgs {
 size_t act_bwd_workspace(int64_t m, int64_t n);
 hipError_t launch_act_bwd(const ActBwdArgs& a, float* dbias, float* workspace, hipStream_t st);
 
-constexpr uint32_t kClipPartials = 1u << 16;                                       // sums of squares, then the factor
+constexpr uint32_t kClipPartials = 1u << 15;                                       // sums of squares, then the factor
 constexpr size_t kClipWorkspaceBytes = kClipPartials * sizeof(double) + 16;
 hipError_t launch_grad_clip(const quartet_grad_tensor* tensors, int64_t count, float max_norm, float* norm, double* workspace, hipStream_t st);
 
