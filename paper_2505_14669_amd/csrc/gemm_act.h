@@ -292,8 +292,9 @@ __device__ __forceinline__ bool store_tile_act(ACC (&acc)[AM][AN], float* wbuf, 
                 const v2u_t o = {bf16_pack2(vv[4 * j], vv[4 * j + 1]), bf16_pack2(vv[4 * j + 2], vv[4 * j + 3])};
                 __builtin_amdgcn_raw_buffer_store_b64(o, td.res, voff, soff, kThroughL2);
             } else {
-                const v4u_t o = {f2u(vv[4 * j]), f2u(vv[4 * j + 1]), f2u(vv[4 * j + 2]), f2u(vv[4 * j + 3])};
+                v4u_t o = {f2u(vv[4 * j]), f2u(vv[4 * j + 1]), f2u(vv[4 * j + 2]), f2u(vv[4 * j + 3])};
                 __builtin_amdgcn_raw_buffer_store_b128(o, td.res, voff, soff, kThroughL2);
+                asm volatile("s_nop 1" : "+v"(o));      // two wait states before the data's registers are written again, as behind every wide store here
             }
         }
     }

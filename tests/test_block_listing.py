@@ -4,7 +4,8 @@ import pytest
 import test_kernel_listing as K
 
 pytestmark = K.pytestmark
-KERNELS = {"mxfp4_act_large_kernelI": 2, "mxfp4_act_tile_kernelILi2ELi4E": 2, "mxfp4_act_tile_kernelILi2ELi2E": 2, "mxfp4_act_twin_kernelI": 2}
+# two result types, four kinds of operands
+KERNELS = {"mxfp4_act_large_kernelI": 8, "mxfp4_act_tile_kernelILi2ELi4E": 8, "mxfp4_act_tile_kernelILi2ELi2E": 8, "mxfp4_act_twin_kernelI": 8}
 
 
 @pytest.fixture(scope="module")
