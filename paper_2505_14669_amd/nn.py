@@ -283,8 +283,8 @@ def clip_grad_norm_(parameters, max_norm):
     if not grads:
         return torch.zeros((), device=parameters[0].device if parameters else None)
     device = grads[0].device
-    if any(g.device != device for g in grads):
-        raise q.QuartetError("all gradients must be on one GPU")
+    if device.type != "cuda" or any(g.device != device for g in grads):
+        raise q.QuartetError("all gradients must be on one GPU: there is no CPU path")
     with torch.cuda.device(device):
         norm = torch.empty((), dtype=torch.float32, device=device)
         size = block.quartet_grad_clip_workspace_bytes()

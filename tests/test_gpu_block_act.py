@@ -44,6 +44,19 @@ def test_backward(m, n, kind, mul):
     backward(rng(m + n), m, n, kind, mul, extra=8 * (m % 2), dmul=True)
 
 
+@pytest.mark.parametrize("dbias", [False, True])
+def test_more_rows_than_blocks_of_the_usual_size(dbias):
+    m, n = 2 ** 25 + 5, 8
+    dy, pre = torch.empty((m, n), dtype=BF16, device=DEV).normal_(generator=rng(5)), torch.empty((m, n), dtype=BF16, device=DEV).normal_(generator=rng(6))
+    dz, db = torch.full((m + 1, n), GUARD, dtype=BF16, device=DEV), torch.empty(n, device=DEV) if dbias else None
+    size = b.quartet_act_bwd_workspace_bytes(m, n)
+    q.check(b.quartet_act_bwd(dy, n, pre, n, None, 0, m, n, 1, dz, n, None, 0, db, torch.empty(size, dtype=torch.uint8, device=DEV), size))
+    want = torch.where(pre > 0, dy, torch.zeros_like(dy))
+    assert torch.equal(dz[:m], want) and bool((dz[m] == GUARD).all())
+    if dbias:      # partial sums of 16 rows and their sums over 2^21 / 32 of them in a thread
+        assert_within(db, want.double().sum(0), (2 ** 16 + 64) * U32 * want.double().abs().sum(0))
+
+
 def test_far_values():
     # gates that are 0 or 1 in every type, squares that overflow
     for kind in ("gelu", "silu", "relu", "none"):

@@ -56,13 +56,21 @@ def test_forward(rows, n, x_dtype, res_dtype, w_dtype):
     assert_within(o["y"], o["want_v"], o["want_v"].abs() * (U16 + 2 * V), "y")
 
 
+def rest_untouched(o, rows, n):
+    """the bytes of the scale buffer that stand for no group"""
+    left = o["scales"].clone()
+    r, g = torch.arange(rows, device=DEV)[:, None], torch.arange(n // 32, device=DEV)[None, :]
+    left[((r // 32) * ((n // 32 + 7) // 8) + g // 8) * 256 + ((g % 2) * 32 + r % 32) * 4 + (g % 8) // 2] = 0xEE
+    return bool((left == 0xEE).all())
+
+
 @pytest.mark.parametrize("rows,n", [(1, 32), (1, 4096), (3, 96), (33, 1376), (40, 2048), (7, 4128), (130, 544), (2, 11008), (1, 32768), (2500, 256)])
 @pytest.mark.parametrize("res_dtype", [None, BF16, F32])
 def test_mxfp8_operand(rows, n, res_dtype):
     o = forward(rng(rows + n), rows, n, BF16, res_dtype, F32, b.QUARTET_FORMAT_MXFP8, scale=3.0, want_y=res_dtype is None)
     v = o["want_v"].view(rows, n // 32, 32)
     e = scale_bytes_of(o["scales"], rows, n // 32).double() - 127
-    assert bool((o["codes"][rows] == 0xEE).all()) and bool((o["scales"][-64:] == 0xEE).all())
+    assert bool((o["codes"][rows] == 0xEE).all()) and rest_untouched(o, rows, n)
     top = v.abs().amax(2)
     # the largest magnitude lies in [2^8, 2^9) scales; next to a power of two the fp32 value may lie on its other side
     assert bool(((torch.ldexp(top, -e) >= 256 * (1 - 2 * V)) & (torch.ldexp(top, -e) < 512 * (1 + 2 * V))).all())
@@ -94,7 +102,7 @@ def test_mxfp4_operand(rows, n, res_dtype, mask):
     s, off = torch.ldexp(h, -e[..., None]), torch.ldexp(off, -e[..., None])
     half = torch.where(s.abs() + off < 2, 0.25, torch.where(s.abs() + off < 4, 0.5, 1.0))
     assert_within(table[both], s.clamp(-6, 6), half + off, "codes")
-    assert bool((o["codes"][rows] == 0xEE).all())
+    assert bool((o["codes"][rows] == 0xEE).all()) and rest_untouched(o, rows, n)
     if mask:
         kept = ((o["mask"][:rows].long()[..., None] >> i) & 1).bool()
         sure = (s.abs() - 6).abs() > off
@@ -162,6 +170,15 @@ def test_rows_far_apart():
     h = x[:, :n].double()
     want = h * (h.square().mean(1, keepdim=True) + 1e-5).rsqrt()
     assert_within(y[:, :n], want, want.abs() * (U16 + 2 * V))
+
+
+@pytest.mark.parametrize("rows,n,fmt", [(4300001, 8, 0), (4200001, 32, 2)])
+def test_more_rows_than_one_dimension_of_blocks(rows, n, fmt):
+    o = forward(rng(6), rows, n, BF16, None, F32, fmt)
+    assert_within(o["y"], o["want_v"], o["want_v"].abs() * (U16 + 2 * V), "y")
+    if fmt:
+        e = scale_bytes_of(o["scales"], rows, 1).double()[:, 0] - 127
+        assert_within(torch.ldexp(o["codes"][:rows].view(torch.float8_e4m3fn).double(), e[:, None]), o["want_v"], o["want_v"].abs() * 2.0 ** -4 * 1.01 + torch.ldexp(torch.ones_like(e), e - 10)[:, None] + o["want_v"].abs().amax(1, keepdim=True) * 0.125 * (o["want_v"].abs() > torch.ldexp(torch.ones_like(e), e)[:, None] * 448))
 
 
 def backward(g, rows, n, h_dtype, w_dtype, dh=True, dx16=False, want_dw=True, extra=0):
