@@ -247,9 +247,11 @@ class _RMSNormFunction(torch.autograd.Function):
             ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
             if rows and (wants_x or need[2]):
                 q.check(block.quartet_rmsnorm_bwd(dy2, ld, h, _dtype_code(h), ld, rows, n, w, _dtype_code(w), rstd, dh2, ld, dx, ld, dx16, ld, dw, ws, size))
-        like = dy
-        gx = _as(dx16 if dx16 is not None else dx, n, like) if need[0] else None
-        return (None if gx is None else gx.to(x_dtype), _as(dx, n, like) if need[1] else None, None if dw is None else dw.to(w.dtype), None)
+        # one tensor object for both where they are the same values: autograd then knows that it is shared and copies it for one of two leaves
+        # (two tensors over one memory it would hand out as two gradients)
+        dstream = None if dx is None else _as(dx, n, dy)
+        gx = dstream if dx16 is None else _as(dx16, n, dy)
+        return (gx.to(x_dtype) if need[0] else None, dstream if need[1] else None, None if dw is None else dw.to(w.dtype), None)
 
 
 class QuartetRMSNorm(torch.nn.Module):
