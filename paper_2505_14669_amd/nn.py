@@ -54,22 +54,52 @@ def _dtype_code(t):
     return q.QUARTET_DTYPE_F32 if t is None or t.dtype == torch.float32 else q.QUARTET_DTYPE_BF16
 
 
-def _rows(t, n):
-    """a tensor [..., n] as dense rows whose distance is a multiple of 8 (the kernels' 16-byte accesses), and that distance"""
-    t = t.reshape(-1, n)
-    if n % 8:
-        wide = torch.empty((t.shape[0], n + 8 - n % 8), dtype=t.dtype, device=t.device)
-        wide[:, :n] = t
-        return wide, wide.shape[1]
-    return t.contiguous(), n
+def _new_rows(shape, dtype, device):
+    """A new tensor [..., n] whose rows lie n, rounded up to a multiple of 8, values apart (the kernels' 16-byte accesses).  It has no wider base: torch
+    refuses changes in place of a function's results that are views."""
+    n = shape[-1]
+    if n % 8 == 0:
+        return torch.empty(shape, dtype=dtype, device=device)
+    strides, step = [1], n + -n % 8
+    for size in reversed(shape[:-1]):
+        strides.insert(0, step)
+        step *= size
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
 
 
-def _new_rows(rows, n, dtype, device):
-    return torch.empty((rows, n + -n % 8), dtype=dtype, device=device)
+def _distance(t):
+    """the distance of the rows of a tensor [..., n] if the kernels take it as it lies, else None"""
+    n = t.shape[-1]
+    if t.is_contiguous() and n % 8 == 0:
+        return n
+    if (n > 1 and t.stride(-1) != 1) or t.data_ptr() % 16:
+        return None
+    distance = step = None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if distance is None:
+            distance = step = stride
+        if stride != step:
+            return None
+        step *= size
+    if distance is None:
+        return n + -n % 8
+    return distance if distance >= n and distance % 8 == 0 else None
 
 
-def _as(t, n, like):
-    return None if t is None else t[:, :n].reshape(like.shape)
+def _rows(t):
+    """a tensor [..., n] as rows that the kernels take, copied if it is not, and their distance"""
+    distance = _distance(t)
+    if distance is None:
+        t = _new_rows(t.shape, t.dtype, t.device).copy_(t)
+        distance = _distance(t)
+    return t, distance
+
+
+def _address(t):
+    """(the binding takes a tensor only where its values lie side by side)"""
+    return None if t is None else t.data_ptr()
 
 
 def _check_tensor(t, name, dtypes, device):
@@ -214,44 +244,44 @@ class _RMSNormFunction(torch.autograd.Function):
                 raise ValueError("residual must have the shape of x")
         rows = x.numel() // n
         with torch.cuda.device(device):
-            x2, ld = _rows(x, n)
-            res2 = None if residual is None else _rows(residual, n)[0]
+            x2, ldx = _rows(x)
+            res2, ldres = (None, 0) if residual is None else _rows(residual)
             w2 = weight.contiguous()
-            h2 = None if residual is None else _new_rows(rows, n, residual.dtype, device)
-            y2, rstd = _new_rows(rows, n, torch.bfloat16, device), torch.empty(rows, dtype=torch.float32, device=device)
+            h = None if residual is None else _new_rows(x.shape, residual.dtype, device)
+            y, rstd, ld = _new_rows(x.shape, torch.bfloat16, device), torch.empty(rows, dtype=torch.float32, device=device), n + -n % 8
             if rows:
-                q.check(block.quartet_rmsnorm_fwd(x2, _dtype_code(x2), ld, res2, ld, rows, n, w2, _dtype_code(w2), float(eps), h2, _dtype_code(h2),
-                                                  ld, y2, ld, block.QUARTET_FORMAT_NONE, None, None, None, rstd))
-        ctx.save_for_backward(x2 if h2 is None else h2, w2, rstd)
-        ctx.like = (x.shape, x.dtype, None if residual is None else residual.dtype, rows, n, ld)
+                q.check(block.quartet_rmsnorm_fwd(_address(x2), _dtype_code(x2), ldx, _address(res2), ldres, rows, n, w2, _dtype_code(w2), float(eps), _address(h),
+                                                  _dtype_code(h), ld, _address(y), ld, block.QUARTET_FORMAT_NONE, None, None, None, rstd))
+        ctx.save_for_backward(x2 if h is None else h, w2, rstd)
+        ctx.like = (x.dtype, rows, n)
         ctx.set_materialize_grads(False)
-        y = _as(y2, n, x)
-        return y, (None if h2 is None else _as(h2, n, x))
+        return y, h
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dh):
         h, w, rstd = ctx.saved_tensors
-        shape, x_dtype, residual_dtype, rows, n, ld = ctx.like
+        x_dtype, rows, n = ctx.like
         if dy is None:
             return (None if dh is None else dh.to(x_dtype)), dh, None, None
         need, device = ctx.needs_input_grad, h.device
         with torch.cuda.device(device):
-            dy2 = _rows(dy.to(torch.bfloat16), n)[0]
-            dh2 = None if dh is None else _rows(dh.to(h.dtype), n)[0]
-            wants_x = need[0] or need[1]
-            dx = _new_rows(rows, n, h.dtype, device) if wants_x else None
-            dx16 = _new_rows(rows, n, torch.bfloat16, device) if wants_x and h.dtype == torch.float32 and x_dtype == torch.bfloat16 else None
+            h, ldh = _rows(h)                   # (what a hook on saved tensors gives back may be laid out otherwise)
+            dy2, lddy = _rows(dy.to(torch.bfloat16))
+            dh2, lddh = (None, 0) if dh is None else _rows(dh.to(h.dtype))
+            wants_x, ld = need[0] or need[1], n + -n % 8
+            dx = _new_rows(h.shape, h.dtype, device) if wants_x else None
+            dx16 = _new_rows(h.shape, torch.bfloat16, device) if wants_x and h.dtype == torch.float32 and x_dtype == torch.bfloat16 else None
             dw = (torch.empty if rows else torch.zeros)(n, dtype=torch.float32, device=device) if need[2] else None
             size = block.quartet_rmsnorm_bwd_workspace_bytes(rows, n)
             ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
             if rows and (wants_x or need[2]):
-                q.check(block.quartet_rmsnorm_bwd(dy2, ld, h, _dtype_code(h), ld, rows, n, w, _dtype_code(w), rstd, dh2, ld, dx, ld, dx16, ld, dw, ws, size))
+                q.check(block.quartet_rmsnorm_bwd(_address(dy2), lddy, _address(h), _dtype_code(h), ldh, rows, n, w, _dtype_code(w), rstd, _address(dh2), lddh,
+                                                  _address(dx), ld, _address(dx16), ld, dw, ws, size))
         # one tensor object for both where they are the same values: autograd then knows that it is shared and copies it for one of two leaves
         # (two tensors over one memory it would hand out as two gradients)
-        dstream = None if dx is None else _as(dx, n, dy)
-        gx = dstream if dx16 is None else _as(dx16, n, dy)
-        return (gx.to(x_dtype) if need[0] else None, dstream if need[1] else None, None if dw is None else dw.to(w.dtype), None)
+        gx = dx if dx16 is None else dx16
+        return (gx.to(x_dtype) if need[0] else None, dx if need[1] else None, None if dw is None else dw.to(w.dtype), None)
 
 
 class QuartetRMSNorm(torch.nn.Module):

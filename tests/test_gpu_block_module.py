@@ -40,3 +40,59 @@ def test_gradients_of_x_and_of_the_stream_accumulate_apart(nn, dtype, n, through
     assert float(nn.clip_grad_norm_([x, res], 1e30)) > 0
     x.grad.zero_()
     assert torch.equal(res.grad, 2 * once)
+
+
+@pytest.mark.parametrize("n", [96, 100])
+def test_results_can_be_changed_in_place(nn, n):
+    g = rng(2)
+    norm = nn.QuartetRMSNorm(n)
+    x, res, dy = new(g, 3, 5, n).requires_grad_(), new(g, 3, 5, n, dtype=F32).requires_grad_(), new(g, 3, 5, n)
+    y, h = norm(x, res)
+    assert y._base is None and h._base is None
+    y.backward(2 * dy)                                     # halving and doubling are exact
+    want = x.grad.clone(), res.grad.clone(), norm.weight.grad.clone()
+    x.grad = res.grad = norm.weight.grad = None
+    y2, h2 = norm(x, res)
+    y2.mul_(2)
+    assert torch.equal(y2, 2 * y)
+    y2.backward(dy)
+    assert all(torch.equal(a, c) for a, c in zip((x.grad, res.grad, norm.weight.grad), want))
+    with torch.no_grad():
+        h3 = norm(x, res)[1]
+        h3 += 1
+        assert torch.equal(h3, h + 1)
+    y4, h4 = norm(x, res)                                  # the backward pass needs h: a changed one is refused there, not used
+    h4.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (y4.float().sum() + h4.sum()).backward()
+
+
+@pytest.mark.parametrize("n", [96, 100])
+def test_saved_tensors_that_come_back_laid_out_otherwise(nn, n):
+    g = rng(3)
+    norm = nn.QuartetRMSNorm(n)
+    x, res, dy = new(g, 3, 5, n).requires_grad_(), new(g, 3, 5, n).requires_grad_(), new(g, 3, 5, n)
+    found = []
+    for hooks in (torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t), torch.autograd.graph.save_on_cpu(),
+                  torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.t().contiguous().t() if t.dim() == 2 else t.transpose(0, -1).contiguous().transpose(0, -1))):
+        x.grad = res.grad = norm.weight.grad = None
+        with hooks:
+            y = norm(x, res)[0]
+            y1 = norm(x)
+        torch.autograd.backward([y, y1], [dy, dy])
+        found.append((x.grad, res.grad, norm.weight.grad))
+    assert all(torch.equal(a, c) for other in found[1:] for a, c in zip(other, found[0]))
+
+
+def test_rows_of_a_wider_tensor(nn):
+    # columns of a wider matrix, one row used many times, a transposed one, a single row: the same bits as their copies
+    g = rng(4)
+    for n in (64, 100, 1):
+        norm = nn.QuartetRMSNorm(n)
+        wide, column = new(g, 6, 4, n + 28), new(g, n, 6, 4)
+        for x in (wide[..., :n], wide[..., 8:8 + n], wide[..., 4:4 + n], wide[:, :1, :n], wide[0, 0, :n], wide[:1, :1, :n].expand(6, 4, n), column.permute(1, 2, 0), wide[::2, 1:, :n]):
+            res = new(g, *x.shape, dtype=F32)
+            want = norm(x.clone(memory_format=torch.contiguous_format), res)
+            assert all(torch.equal(a, c) for a, c in zip(norm(x, res), want))
+            want = norm(x.clone(memory_format=torch.contiguous_format), x.clone(memory_format=torch.contiguous_format))
+            assert all(torch.equal(a, c) for a, c in zip(norm(x, x), want))
