@@ -116,7 +116,7 @@ class _EpilogueFunction(torch.autograd.Function):
     """a(x W^T + bias) * multiplier + residual: the layer's operands, its product with the epilogue, and both backward passes."""
 
     @staticmethod
-    def forward(ctx, x, weight, bias, multiplier, residual, seed, rounding, hadamard_block, activation):
+    def forward(ctx, x, weight, bias, multiplier, residual, seed, rounding, hadamard_block, activation, graph):
         device = x.device
         _check_tensor(x, "x", (torch.bfloat16,), device)
         _check_tensor(weight, "weight", (torch.bfloat16,), device)
@@ -151,7 +151,8 @@ class _EpilogueFunction(torch.autograd.Function):
             else:
                 q.check(q.quartet_quant_fwd_block(x2, tokens, inf, inf, 0, hadamard_block, *operands[:3]))
                 q.check(q.quartet_quant_fwd_block(w2, out, inf, inf, 0, hadamard_block, *operands[3:]))
-            track = any(ctx.needs_input_grad)
+            # z is kept for a backward pass only (needs_input_grad is true of a weight under no_grad too; in here no_grad always holds, so the caller says)
+            track = graph and any(ctx.needs_input_grad[:4])            # (the residual's gradient is the result's)
             pre = torch.empty((tokens, out), dtype=torch.bfloat16, device=device) if track and (activation or mul2 is not None) else None
             y = torch.empty(shape, dtype=torch.bfloat16 if residual is None else residual.dtype, device=device)
             q.check(block.quartet_mxfp4_gemm_act(operands[0], operands[1], operands[3], operands[4], tokens, out, inf, 1.0, bias2, _dtype_code(bias2),
@@ -187,7 +188,7 @@ class _EpilogueFunction(torch.autograd.Function):
                 size = q.quartet_linear_workspace_bytes_block(tokens, inf, out, hadamard_block)
                 ws = torch.empty(max(256, size), dtype=torch.uint8, device=device)
                 q.check(q.quartet_linear_bwd_block(dz, tokens, inf, out, hadamard_block, *operands, seed, rounding, dx, dw, q.QUARTET_DTYPE_BF16, ws, size))
-        return (dx, dw, None if dbias is None else dbias.to(bias_dtype), dmul, dy.to(residual_dtype) if need[4] else None, None, None, None, None)
+        return (dx, dw, None if dbias is None else dbias.to(bias_dtype), dmul, dy.to(residual_dtype) if need[4] else None, None, None, None, None, None)
 
 
 class QuartetLinear(torch.nn.Module):
@@ -222,7 +223,7 @@ class QuartetLinear(torch.nn.Module):
         weight = self.weight.to(torch.bfloat16)
         if self.activation != "none" or multiplier is not None or residual is not None:
             return _EpilogueFunction.apply(x, weight, self.bias, multiplier, residual, seed, self.rounding, self.hadamard_block,
-                                           block.ACTIVATIONS[self.activation])
+                                           block.ACTIVATIONS[self.activation], torch.is_grad_enabled())
         y = QuartetLinearFunction.apply(x, weight, seed, self.rounding, self.hadamard_block)
         return y if self.bias is None else y + self.bias
 

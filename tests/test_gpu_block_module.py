@@ -2,6 +2,7 @@
 buffer, inference without a graph."""
 import pytest
 import torch
+import torch.utils.checkpoint
 
 from block_util import BF16, DEV, F32, rng
 
@@ -96,3 +97,33 @@ def test_rows_of_a_wider_tensor(nn):
             assert all(torch.equal(a, c) for a, c in zip(norm(x, res), want))
             want = norm(x.clone(memory_format=torch.contiguous_format), x.clone(memory_format=torch.contiguous_format))
             assert all(torch.equal(a, c) for a, c in zip(norm(x, x), want))
+
+
+def calls(monkeypatch, nn, name):
+    """the argument lists of the binding's call `name` from now on"""
+    seen, real = [], getattr(nn.block, name)
+    monkeypatch.setattr(nn.block, name, lambda *args: (seen.append(args), real(*args))[1])
+    return seen
+
+
+def test_inference_keeps_nothing_for_a_backward_pass(nn, monkeypatch):
+    g = rng(5)
+    lin, x, up = nn.QuartetLinear(64, 96, activation="silu"), new(g, 32, 64), new(g, 32, 96)
+    seen = calls(monkeypatch, nn, "quartet_mxfp4_gemm_act")
+    pre = 16                                              # z's place among the arguments
+    y = lin(x, multiplier=up)
+    with torch.no_grad():
+        y_no_grad = lin(x, multiplier=up)
+    with torch.inference_mode():
+        y_inference = lin(x, multiplier=up)
+    assert [args[pre] is not None for args in seen] == [True, False, False]
+    assert torch.equal(y, y_no_grad) and torch.equal(y, y_inference)
+    y = torch.utils.checkpoint.checkpoint(lambda t: lin(t, multiplier=up), x.requires_grad_(), use_reentrant=True)      # first without a graph, then with one
+    assert [args[pre] is not None for args in seen[3:]] == [False]
+    y.float().sum().backward()
+    assert [args[pre] is not None for args in seen[3:]] == [False, True] and bool(torch.isfinite(x.grad).all())
+    # a frozen layer: what goes along the residual needs no z
+    lin.requires_grad_(False)
+    res = new(g, 32, 96, dtype=F32).requires_grad_()
+    lin(x.detach(), multiplier=up, residual=res).backward(new(g, 32, 96, dtype=F32))
+    assert seen[-1][pre] is None and res.grad is not None
