@@ -177,8 +177,8 @@ class _EpilogueFunction(torch.autograd.Function):
                 dz = dy2 if plain else torch.empty_like(dy2)
                 dmul = torch.empty(dy.shape, dtype=torch.bfloat16, device=device) if need[3] else None
                 dbias = torch.empty(out, dtype=torch.float32, device=device) if need[2] else None
-                size = block.quartet_act_bwd_workspace_bytes(tokens, out)
-                ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
+                size = block.quartet_act_bwd_workspace_bytes(tokens, out) if need[2] else 0
+                ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
                 if dbias is not None or dmul is not None or not plain:
                     q.check(block.quartet_act_bwd(dy2, out, pre, out, mul, out, tokens, out, activation, None if plain else dz, out, dmul, out, dbias,
                                                   ws, size))
@@ -274,8 +274,8 @@ class _RMSNormFunction(torch.autograd.Function):
             dx = _new_rows(h.shape, h.dtype, device) if wants_x else None
             dx16 = _new_rows(h.shape, torch.bfloat16, device) if wants_x and h.dtype == torch.float32 and x_dtype == torch.bfloat16 else None
             dw = (torch.empty if rows else torch.zeros)(n, dtype=torch.float32, device=device) if need[2] else None
-            size = block.quartet_rmsnorm_bwd_workspace_bytes(rows, n)
-            ws = torch.empty(max(16, size), dtype=torch.uint8, device=device)
+            size = block.quartet_rmsnorm_bwd_workspace_bytes(rows, n) if need[2] else 0
+            ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
             if rows and (wants_x or need[2]):
                 q.check(block.quartet_rmsnorm_bwd(_address(dy2), lddy, _address(h), _dtype_code(h), ldh, rows, n, w, _dtype_code(w), rstd, _address(dh2), lddh,
                                                   _address(dx), ld, _address(dx16), ld, dw, ws, size))

@@ -127,3 +127,19 @@ def test_inference_keeps_nothing_for_a_backward_pass(nn, monkeypatch):
     res = new(g, 32, 96, dtype=F32).requires_grad_()
     lin(x.detach(), multiplier=up, residual=res).backward(new(g, 32, 96, dtype=F32))
     assert seen[-1][pre] is None and res.grad is not None
+
+
+def test_workspaces_only_for_sums_over_the_rows(nn, monkeypatch):
+    g = rng(6)
+    x, up, dy = new(g, 64, 128).requires_grad_(), new(g, 64, 96).requires_grad_(), new(g, 64, 96)
+    for bias in (False, True):
+        lin, seen = nn.QuartetLinear(128, 96, bias=bias, activation="gelu"), calls(monkeypatch, nn, "quartet_act_bwd")
+        lin(x, multiplier=up).backward(dy)
+        size = nn.block.quartet_act_bwd_workspace_bytes(64, 96)
+        assert size > 0 and (seen[-1][14] is not None, seen[-1][15]) == ((True, size) if bias else (False, 0))
+    for weight in (True, False):
+        norm, seen = nn.QuartetRMSNorm(128).requires_grad_(weight), calls(monkeypatch, nn, "quartet_rmsnorm_bwd")
+        norm(x).backward(new(g, 64, 128))
+        size = nn.block.quartet_rmsnorm_bwd_workspace_bytes(64, 128)
+        assert size > 0 and (seen[-1][17] is not None, seen[-1][18]) == ((True, size) if weight else (False, 0))
+    assert bool(torch.isfinite(x.grad).all()) and bool(torch.isfinite(up.grad).all())
