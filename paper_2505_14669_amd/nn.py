@@ -70,9 +70,11 @@ def _new_rows(shape, dtype, device):
 def _distance(t):
     """the distance of the rows of a tensor [..., n] if the kernels take it as it lies, else None"""
     n = t.shape[-1]
+    if t.data_ptr() % 16:
+        return None
     if t.is_contiguous() and n % 8 == 0:
         return n
-    if (n > 1 and t.stride(-1) != 1) or t.data_ptr() % 16:
+    if n > 1 and t.stride(-1) != 1:
         return None
     distance = step = None
     for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
@@ -95,6 +97,14 @@ def _rows(t):
         t = _new_rows(t.shape, t.dtype, t.device).copy_(t)
         distance = _distance(t)
     return t, distance
+
+
+def _dense(t):
+    """a tensor (or None) with its values side by side from a multiple of 16 bytes on, copied if it is not: a piece of a program's buffer may start anywhere"""
+    if t is None:
+        return None
+    t = t.contiguous()
+    return t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t
 
 
 def _address(t):
@@ -139,8 +149,7 @@ class _EpilogueFunction(torch.autograd.Function):
             if tuple(bias.shape) != (out,):
                 raise ValueError(f"bias must have {out} values")
         with torch.cuda.device(device):
-            x2, w2 = x.reshape(tokens, inf).contiguous(), weight.contiguous()
-            bias2, mul2, res2 = (None if t is None else t.contiguous() for t in (bias, multiplier, residual))
+            x2, w2, bias2, mul2, res2 = _dense(x), _dense(weight), _dense(bias), _dense(multiplier), _dense(residual)
             byte = dict(dtype=torch.uint8, device=device)
             operands = []
             for t, rows in ((x2, tokens), (w2, out)):
@@ -171,7 +180,7 @@ class _EpilogueFunction(torch.autograd.Function):
         device, need = dy.device, ctx.needs_input_grad
         dx = dw = dbias = dmul = None
         with torch.cuda.device(device):
-            dz = dy2 = dy.reshape(tokens, out).to(torch.bfloat16).contiguous()
+            dz = dy2 = _dense(dy.reshape(tokens, out).to(torch.bfloat16))
             if pre is not None or need[2]:
                 plain = activation == 0 and mul is None
                 dz = dy2 if plain else torch.empty_like(dy2)
@@ -247,7 +256,7 @@ class _RMSNormFunction(torch.autograd.Function):
         with torch.cuda.device(device):
             x2, ldx = _rows(x)
             res2, ldres = (None, 0) if residual is None else _rows(residual)
-            w2 = weight.contiguous()
+            w2 = _dense(weight)
             h = None if residual is None else _new_rows(x.shape, residual.dtype, device)
             y, rstd, ld = _new_rows(x.shape, torch.bfloat16, device), torch.empty(rows, dtype=torch.float32, device=device), n + -n % 8
             if rows:

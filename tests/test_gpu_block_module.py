@@ -143,3 +143,48 @@ def test_workspaces_only_for_sums_over_the_rows(nn, monkeypatch):
         size = nn.block.quartet_rmsnorm_bwd_workspace_bytes(64, 128)
         assert size > 0 and (seen[-1][17] is not None, seen[-1][18]) == ((True, size) if weight else (False, 0))
     assert bool(torch.isfinite(x.grad).all()) and bool(torch.isfinite(up.grad).all())
+
+
+def anywhere(t, leaf=True):
+    """a copy of t in the middle of a buffer, at an odd element"""
+    buffer = torch.zeros(t.numel() + 16, dtype=t.dtype, device=DEV)
+    view = buffer[3:3 + t.numel()].view(t.shape).copy_(t)
+    assert view.data_ptr() % 16
+    return view.detach().requires_grad_() if leaf else view
+
+
+def test_layer_takes_tensors_that_start_anywhere(nn):
+    # pieces of flat buffers (sharded parameters, packed activations): the same bits as tensors of their own
+    g = rng(7)
+    x, up, res, dy = new(g, 32, 64), new(g, 32, 96), new(g, 32, 96, dtype=F32), new(g, 32, 96, dtype=F32)
+    lin = nn.QuartetLinear(64, 96, bias=True, rounding=1, activation="silu")
+    with torch.no_grad():
+        lin.bias.copy_(new(g, 96))
+    found = []
+    for place in (lambda t: t.clone().requires_grad_(), anywhere):
+        leaves = [place(t) for t in (x, up, res)]
+        lin.weight.data, lin.bias.data = place(lin.weight.data).detach(), place(lin.bias.data).detach()
+        lin.weight.grad = lin.bias.grad = None
+        lin.calls = 0                                          # (a call's number is part of the backward pass's random signs)
+        y = lin(leaves[0], multiplier=leaves[1], residual=leaves[2])
+        y.backward(place(dy).detach())
+        y16 = lin(leaves[0])
+        y16.backward(place(up).detach())
+        found.append([y, y16, *(t.grad for t in leaves), lin.weight.grad, lin.bias.grad])
+    assert all(torch.equal(a, c) for a, c in zip(*found))
+
+
+@pytest.mark.parametrize("n", [64, 101])
+def test_norm_takes_tensors_that_start_anywhere(nn, n):
+    g = rng(8)
+    x, res, dy, dh = new(g, 3, 5, n), new(g, 3, 5, n, dtype=F32), new(g, 3, 5, n), new(g, 3, 5, n, dtype=F32)
+    norm, found = nn.QuartetRMSNorm(n), []
+    with torch.no_grad():
+        norm.weight.copy_(new(g, n, dtype=F32))
+    for place in (lambda t: t.clone().requires_grad_(), anywhere):
+        leaves = [place(t) for t in (x, res)]
+        norm.weight.data, norm.weight.grad = place(norm.weight.data).detach(), None
+        y, h = norm(*leaves)
+        torch.autograd.backward([y, h], [place(dy).detach(), place(dh).detach()])
+        found.append([y, h, *(t.grad for t in leaves), norm.weight.grad])
+    assert all(torch.equal(a, c) for a, c in zip(*found))
