@@ -210,8 +210,16 @@ hipError_t launch_grad_clip(const quartet_grad_tensor* tensors, int64_t count, f
     };
     float* factor = reinterpret_cast<float*>(workspace + kClipPartials);
     const bool few = all <= kFew;
-    // What the memory-side cache cannot hold goes past it in the second pass (us, through the caches / past them: 202 M values 300 / 260, 51 M fp32 118 / 99).
-    const bool past = all * ((uint64_t)kChunk << shift) >= ((uint64_t)32 << 20);
+    // Copies go past the memory-side cache (256 MiB) where it cannot hold them and their gradients: plain accesses would push out what the second pass still reads
+    // (us, through / past: bf16 to fp32 64 + 128 MiB 48.8 / 48.8, 96 + 192 69.4 / 68.2, 128 + 256 91.5 / 86.9, 256 + 512 185 / 167; fp32 to bf16 192 + 96 81.6 / 78.7;
+    // fp32 128 + 128 64.8 / 64.9).  In place nothing is pushed out, each line is written where it was read: through it at every size (fp32 32 MiB 23.0 / 27.9, 256 MiB
+    // 122.9 / 127.4, 512 MiB 294 / 306, bf16 64 MiB 42.3 / 45.4).
+    uint64_t copied = 0u;
+    for (int64_t i = 0; i < count; ++i) {
+        const quartet_grad_tensor& t = tensors[i];
+        if (t.size > 0 && t.grad != t.out) copied += (uint64_t)t.size * ((t.grad_dtype == QUARTET_DTYPE_F32 ? 4u : 2u) + (t.out_dtype == QUARTET_DTYPE_F32 ? 4u : 2u));
+    }
+    const bool past = copied >= ((uint64_t)256 << 20);
     ClipList l;
     double* partial = workspace;
     for (int64_t at = 0; at < count; partial += l.chunks) {
