@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import test_gpu_block_act as A
-from block_util import BF16, DEV, F32, GUARD, rng
+import test_gpu_block_norm as N
+from block_util import BF16, DEV, F32, GUARD, U32, b, code, q, quantized, rng
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +39,61 @@ def test_clip_of_more_chunks_than_the_workspace_has_sums_for(dtype):
     assert torch.equal(flat[:3], ends[0]) and torch.equal(flat[at:], ends[1])
     copies = [torch.empty(s, dtype=F32, device=DEV) for s in sizes]
     A.check_clip(views, copies, 0.5)
+
+
+# 1024 rows and more: blocks go by the tiles of 32 rows of the scales, 4, 2 or 1 rows a block
+TILED = [(1024, 480), (1100, 1376), (1057, 992), (1030, 4096), (1025, 8224), (2050, 512)]
+
+
+@pytest.mark.parametrize("rows,n", TILED)
+@pytest.mark.parametrize("res_dtype", [None, F32])
+def test_norm_operands_by_scale_tile(rows, n, res_dtype):
+    N.test_mxfp8_operand(rows, n, res_dtype)
+    N.test_mxfp4_operand(rows, n, res_dtype, True)
+
+
+def test_norm_results_that_the_cache_cannot_hold():
+    # codes of 64 MiB and more, bf16 results of 256 MiB and more; rows of sixteen waves and of one
+    for rows, n in ((32900, 4128), (1050000, 128)):
+        N.test_mxfp4_operand(rows, n, None, False)
+        torch.cuda.empty_cache()
+        N.test_forward(rows, n, BF16, BF16, F32)
+        torch.cuda.empty_cache()
+    N.test_mxfp8_operand(16500, 4128, BF16)
+    torch.cuda.empty_cache()
+
+
+# one, two, four and sixteen waves a row, sixteen with two and four chunks a lane; widths with and without an incomplete chunk
+@pytest.mark.parametrize("rows,n,h_dtype,dh", [(270001, 100, F32, True), (130003, 520, BF16, True), (27001, 1003, F32, True), (6601, 4100, F32, True),
+                                               (16500, 4096, BF16, False), (3301, 8203, F32, True), (1650, 16392, F32, True)])
+def test_norm_backward_of_what_the_cache_cannot_hold(rows, n, h_dtype, dh):
+    assert rows * n * (2 + (4 if h_dtype == F32 else 2) * (2 if dh else 1)) >= 256 << 20
+    N.test_backward(rows, n, h_dtype, F32, dh)
+    torch.cuda.empty_cache()
+
+
+# the in-block split's kernels, tiles of every size, ragged ones, results of 256 MiB and more
+@pytest.mark.parametrize("m,n,k", [(1, 8, 64), (24, 11008, 512), (96, 416, 256), (600, 768, 1024), (1003, 5632, 2048), (2100, 4448, 320), (4096, 2048, 2048),
+                                   (8192, 4096, 512), (16500, 8200, 288)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_without_an_epilogue_it_is_the_plain_product_to_the_bit(m, n, k, out):
+    # same sizes, same kernel, same order of sums, without a forced plan too
+    a, a_scales, _ = quantized(rng(3), m, k)
+    w, w_scales, _ = quantized(rng(4), n, k)
+    d, want = torch.empty((m, n), dtype=out, device=DEV), torch.empty((m, n), dtype=out, device=DEV)
+    q.check(q.quartet_mxfp4_gemm(a, a_scales, w, w_scales, m, n, k, 0.75, want, code(want), n))
+    q.check(b.quartet_mxfp4_gemm_act(a, a_scales, w, w_scales, m, n, k, 0.75, None, 0, 0, None, 0, None, 0, 0, None, 0, d, code(d), n))
+    assert torch.equal(d, want)
+
+
+# What the norm's rounding adds up to, in half steps u of fp32: a lane's eight squares are rounded once each and added in a tree of three, all positive: 4 u,
+# halved by the root; the sum over the lanes, the quotient and the root are in 64 bits, rounded to fp32 once: rstd within 3 u, v within 5 u.
+@pytest.mark.parametrize("rows,n", [(3, 8), (33, 1376), (130, 1003), (2, 8192), (2, 32768), (700, 4096)])
+def test_norm_statistic_in_64_bits(monkeypatch, rows, n):
+    monkeypatch.setattr(N, "RSTD", 3.01 * U32)
+    monkeypatch.setattr(N, "V", 5.02 * U32)
+    for types in ((BF16, None, F32), (F32, F32, F32), (BF16, F32, BF16)):
+        N.test_forward(rows, n, *types)
+    if n % 32 == 0:
+        N.test_mxfp8_operand(rows, n, F32)
+        N.test_mxfp4_operand(rows, n, F32, True)

@@ -188,3 +188,22 @@ def test_norm_takes_tensors_that_start_anywhere(nn, n):
         torch.autograd.backward([y, h], [place(dy).detach(), place(dh).detach()])
         found.append([y, h, *(t.grad for t in leaves), norm.weight.grad])
     assert all(torch.equal(a, c) for a, c in zip(*found))
+
+
+@pytest.mark.parametrize("hadamard_block,t,i,o", [(32, 96, 160, 64), (64, 128, 192, 64), (128, 128, 256, 384), (256, 256, 512, 256)])
+@pytest.mark.parametrize("kind", ["none", "relu", "gelu", "silu"])
+def test_gradients_are_the_plain_layers_for_the_epilogues_gradient(nn, kind, hadamard_block, t, i, o):
+    # dz from the operator's own call on the plain product's result; with it the plain layer's backward pass must give the same bits for x and for the weight
+    g = rng(9)
+    x, up, res, dy = new(g, t, i), new(g, t, o), new(g, t, o), new(g, t, o, scale=0.1)
+    lin = nn.QuartetLinear(i, o, seed=5, rounding=0, hadamard_block=hadamard_block, activation=kind)
+    x1, x2, up1 = x.clone().requires_grad_(), x.clone().requires_grad_(), up.clone().requires_grad_()
+    y = lin(x1, multiplier=up1, residual=res)
+    y.backward(dy)
+    got, lin.weight.grad = lin.weight.grad, None
+    z = nn.QuartetLinearFunction.apply(x2, lin.weight, (lin.base_seed << 48) | (lin.layer_id << 32), 0, hadamard_block)
+    dz, dup = torch.empty_like(dy), torch.empty_like(dy)
+    nn.q.check(nn.block.quartet_act_bwd(dy, o, z.detach(), o, up, o, t, o, nn.block.ACTIVATIONS[kind], dz, o, dup, o, None, None, 0))
+    z.backward(dz)
+    assert torch.equal(x1.grad, x2.grad) and torch.equal(got, lin.weight.grad) and torch.equal(up1.grad, dup)
+    assert bool((got != 0).any()) and bool((x2.grad != 0).any())
