@@ -9,8 +9,8 @@
  * launched; the same return values.  Empty calls (a zero size) launch nothing where there is nothing to write.  Results do not depend on
  * anything but the arguments: there are no atomics, two calls on the same inputs give the same bits.
  *
- * Number formats: sums, statistics and activations are formed in fp32 (the gradient norm in fp64) and every result is rounded once, to nearest
- * even, where it is stored.  Infinities and NaN pass through the arithmetic as IEEE rules have it, except where a result is an MX
+ * Number formats: sums and activations are formed in fp32 (the squares of the norm's statistic and of the gradient norm, and their sums, in fp64) and every
+ * result is rounded once, to nearest even, where it is stored.  Infinities and NaN pass through the arithmetic as IEEE rules have it, except where a result is an MX
  * operand (an E4M3 element saturates at 448, an E2M1 element at 6; a NaN makes its group's codes unspecified).
  */
 #ifndef QUARTET_BLOCK_H

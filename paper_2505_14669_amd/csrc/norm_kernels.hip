@@ -129,8 +129,9 @@ __device__ __forceinline__ uint32_t tile_row(uint32_t b) {
     return ((i / PER) * 8u + (b & 7u)) * 32u + (i % PER) * RPB;
 }
 
-// The sum of squares over the row in 64 bits (the lanes' own eight in 32): what is left of rounding in the statistic is its own last one, and a code that lies
-// next to the middle of two falls as the exact value does about twice as often as with 32 bits.
+// The row's squares and their sum in 64 bits (no value of fp32 has a square outside them): the statistic is rounded once, to fp32.  Rounding of the values behind
+// it still moves codes next to the middle of two; against the exact operand 25 of 128.6 M E2M1 codes and 370 of 671 M E4M3 codes fall otherwise (with everything in
+// 32 bits, in torch's order, 70 and 488).  Beside squares in 32 bits it costs 0.5 % (16384 x 4096 into MXFP8 84.0 us for 83.0, into bf16 93.3 for 93.2).
 template <int WPR>
 __device__ __forceinline__ double row_sum64(double s, double* meet, uint32_t slot, uint32_t sub, uint32_t lane) {
     s = wave_sum64(s);
@@ -201,10 +202,8 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
             }
             if (a.h) store8<true>(h_row, a.h_f32, col[j], tail[j], v[j]);
         }
-        float t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = v[j][i] * v[j][i];
-        part += (double)(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
+        for (int i = 0; i < 8; ++i) part = __builtin_fma((double)v[j][i], (double)v[j][i], part);
     }
     const float rstd = rsqrt_once(row_sum64<WPR>(part, meet, slot, sub, lane) * a.inv_n + (double)a.eps);
     if (a.rstd && in && sub == 0u && lane == 0u) a.rstd[row] = rstd;

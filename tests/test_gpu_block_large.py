@@ -5,7 +5,7 @@ import torch
 
 import test_gpu_block_act as A
 import test_gpu_block_norm as N
-from block_util import BF16, DEV, F32, GUARD, U32, b, code, q, quantized, rng
+from block_util import BF16, DEV, F32, GUARD, HALF, U32, assert_within, b, code, matrix, q, quantized, rng
 
 pytestmark = pytest.mark.gpu
 
@@ -86,14 +86,34 @@ def test_without_an_epilogue_it_is_the_plain_product_to_the_bit(m, n, k, out):
     assert torch.equal(d, want)
 
 
-# What the norm's rounding adds up to, in half steps u of fp32: a lane's eight squares are rounded once each and added in a tree of three, all positive: 4 u,
-# halved by the root; the sum over the lanes, the quotient and the root are in 64 bits, rounded to fp32 once: rstd within 3 u, v within 5 u.
+# What the norm's rounding adds up to, in half steps u of fp32: squares, sum, quotient and root are in 64 bits and rounded to fp32 once: rstd within u, v, two
+# products more, within 3 u (and what is smaller by 2^-24 and more).
 @pytest.mark.parametrize("rows,n", [(3, 8), (33, 1376), (130, 1003), (2, 8192), (2, 32768), (700, 4096)])
 def test_norm_statistic_in_64_bits(monkeypatch, rows, n):
-    monkeypatch.setattr(N, "RSTD", 3.01 * U32)
-    monkeypatch.setattr(N, "V", 5.02 * U32)
+    monkeypatch.setattr(N, "RSTD", 1.01 * U32)
+    monkeypatch.setattr(N, "V", 3.02 * U32)
     for types in ((BF16, None, F32), (F32, F32, F32), (BF16, F32, BF16)):
         N.test_forward(rows, n, *types)
     if n % 32 == 0:
         N.test_mxfp8_operand(rows, n, F32)
         N.test_mxfp4_operand(rows, n, F32, True)
+
+
+@pytest.mark.parametrize("scale,eps", [(1e20, 1e-5), (1e30, 1e-5), (1e-25, 0.0), (1e-30, 0.0)])
+@pytest.mark.parametrize("rows,n", [(3, 100), (5, 4096), (2, 16392)])
+def test_norm_of_values_whose_squares_fp32_cannot_hold(rows, n, scale, eps):
+    # the mean is finite and not 0, so is everything behind it
+    for dtype in (BF16, F32):
+        o = N.forward(rng(5), rows, n, dtype, None, F32, eps=eps, scale=scale)
+        assert_within(o["rstd"][:rows], o["want_rstd"], o["want_rstd"] * N.RSTD, "rstd")
+        assert_within(o["y"], o["want_v"], o["want_v"].abs() * (HALF[BF16] + 2 * N.V), "y")
+        # the backward pass from that statistic: bounds as in the norm's own test
+        dy, h, w, rstd, ld = matrix(rng(6), rows, n, BF16, 0.01), o["x"], o["w"], o["rstd"][:rows], o["x"].shape[1]
+        dx, dw, size = torch.empty_like(h), torch.empty(n, device=DEV), b.quartet_rmsnorm_bwd_workspace_bytes(rows, n)
+        q.check(b.quartet_rmsnorm_bwd(dy, ld, h, code(h), ld, rows, n, w, 0, rstd, None, 0, dx, ld, None, 0, dw, torch.empty(size, dtype=torch.uint8, device=DEV), size))
+        gd, hd, r = dy[:, :n].double() * w.double(), h[:, :n].double(), rstd.double()[:, None]
+        gh = gd * hd
+        want = r * (gd - hd * r * r * gh.mean(1, keepdim=True))
+        assert_within(dx[:, :n], want, 36 * U32 * hd.abs() * r ** 3 * gh.abs().mean(1, keepdim=True) + 6 * U32 * r * gd.abs() + want.abs() * HALF[dtype], "dx")
+        terms = dy[:, :n].double() * hd * r
+        assert_within(dw, terms.sum(0), (rows / 64 + 200) * U32 * terms.abs().sum(0), "dw")
