@@ -148,6 +148,10 @@ class _EpilogueFunction(torch.autograd.Function):
             _check_tensor(bias, "bias", _ANY, device)
             if tuple(bias.shape) != (out,):
                 raise ValueError(f"bias must have {out} values")
+        ctx.call = (tokens, inf, out, seed, rounding, hadamard_block, activation)
+        ctx.like = (x.shape, None if bias is None else bias.dtype, None if residual is None else residual.dtype)
+        if inf and not tokens * out:                # no tokens or no features: nothing to multiply, and the library takes no address of nothing
+            return torch.empty(shape, dtype=torch.bfloat16 if residual is None else residual.dtype, device=device)
         with torch.cuda.device(device):
             x2, w2, bias2, mul2, res2 = _dense(x), _dense(weight), _dense(bias), _dense(multiplier), _dense(residual)
             byte = dict(dtype=torch.uint8, device=device)
@@ -167,17 +171,19 @@ class _EpilogueFunction(torch.autograd.Function):
             q.check(block.quartet_mxfp4_gemm_act(operands[0], operands[1], operands[3], operands[4], tokens, out, inf, 1.0, bias2, _dtype_code(bias2),
                                                  activation, mul2, out, res2, _dtype_code(res2), out, pre, out, y, _dtype_code(y), out))
         ctx.save_for_backward(pre, mul2, *operands)
-        ctx.call = (tokens, inf, out, seed, rounding, hadamard_block, activation)
-        ctx.like = (x.shape, None if bias is None else bias.dtype, None if residual is None else residual.dtype)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        pre, mul, *operands = ctx.saved_tensors
         tokens, inf, out, seed, rounding, hadamard_block, activation = ctx.call
         x_shape, bias_dtype, residual_dtype = ctx.like
         device, need = dy.device, ctx.needs_input_grad
+        if not tokens * out:
+            zeros = [torch.zeros(s, dtype=t, device=device) if n else None
+                     for s, t, n in zip((x_shape, (out, inf), (out,), dy.shape), (torch.bfloat16, torch.bfloat16, bias_dtype, torch.bfloat16), need)]
+            return (*zeros, dy.to(residual_dtype) if need[4] else None, None, None, None, None, None)
+        pre, mul, *operands = ctx.saved_tensors
         dx = dw = dbias = dmul = None
         with torch.cuda.device(device):
             dz = dy2 = _dense(dy.reshape(tokens, out).to(torch.bfloat16))

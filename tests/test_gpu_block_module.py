@@ -207,3 +207,18 @@ def test_gradients_are_the_plain_layers_for_the_epilogues_gradient(nn, kind, had
     z.backward(dz)
     assert torch.equal(x1.grad, x2.grad) and torch.equal(got, lin.weight.grad) and torch.equal(up1.grad, dup)
     assert bool((got != 0).any()) and bool((x2.grad != 0).any())
+
+
+@pytest.mark.parametrize("shape", [(0, 64), (3, 0, 64)])
+def test_layer_with_an_epilogue_over_no_tokens(nn, shape):
+    # a batch without tokens (an expert that got none): an empty result, gradients of zeros
+    lin = nn.QuartetLinear(64, 96, bias=True, activation="silu")
+    x, res = torch.empty(shape, dtype=BF16, device=DEV).requires_grad_(), torch.empty((*shape[:-1], 96), device=DEV).requires_grad_()
+    up = torch.empty((*shape[:-1], 96), dtype=BF16, device=DEV).requires_grad_()
+    y = lin(x, multiplier=up, residual=res)
+    assert y.shape == (*shape[:-1], 96) and y.dtype == F32
+    y.sum().backward()
+    assert x.grad.shape == x.shape and up.grad.shape == up.shape and res.grad.dtype == F32
+    assert lin.weight.grad.shape == (96, 64) and bool((lin.weight.grad == 0).all()) and lin.bias.grad.shape == (96,) and bool((lin.bias.grad == 0).all())
+    with torch.no_grad():
+        assert lin(x).shape == y.shape
