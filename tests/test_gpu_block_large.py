@@ -117,3 +117,23 @@ def test_norm_of_values_whose_squares_fp32_cannot_hold(rows, n, scale, eps):
         assert_within(dx[:, :n], want, 36 * U32 * hd.abs() * r ** 3 * gh.abs().mean(1, keepdim=True) + 6 * U32 * r * gd.abs() + want.abs() * HALF[dtype], "dx")
         terms = dy[:, :n].double() * hd * r
         assert_within(dw, terms.sum(0), (rows / 64 + 200) * U32 * terms.abs().sum(0), "dw")
+
+
+@pytest.mark.parametrize("variant", [-1, 0, 1, 2, 22])
+@pytest.mark.parametrize("m,n", [(1, 8), (5, 256), (40, 4096), (129, 300), (200, 512), (257, 1001)])
+def test_product_leaves_the_rows_behind_the_last_one(variant, m, n):
+    # a tile has up to 256 rows; every row that it could reach lies in the buffer
+    k = 96
+    a, a_scales, _ = quantized(rng(7), m, k)
+    w, w_scales, _ = quantized(rng(8), n, k)
+    ld = (n + 7) // 8 * 8 + 8
+    try:
+        q.check(q.quartet_debug_set_gemm_plan(variant, 0))
+        for out in (BF16, F32):
+            d, pre = (torch.full((m + 520, ld), GUARD, dtype=t, device=DEV) for t in (out, BF16))
+            res, up = (torch.ones((m + 520, ld), dtype=t, device=DEV) for t in (F32, BF16))
+            q.check(b.quartet_mxfp4_gemm_act(a, a_scales, w, w_scales, m, n, k, 1.0, None, 0, 3, up, ld, res, 0, ld, pre, ld, d, code(d), ld))
+            for t in (d, pre):
+                assert bool((t[m:] == GUARD).all()) and bool((t[:m, n:] == GUARD).all()) and not bool((t[:m, :n] == GUARD).any())
+    finally:
+        q.quartet_debug_set_gemm_plan(-1, 0)
