@@ -43,8 +43,9 @@ extern "C" {
  * [m x ldres] of residual_dtype or NULL; pre: where z is stored as bf16 [m x ldpre] for quartet_act_bwd, or NULL.  The activation works
  * on z in fp32, not on its stored copy.  Leading dimensions of the matrices that are given lie between n and 2^21.  multiplier or residual
  * may be d itself (same type and leading dimension): every element is read before it is written.  Other overlaps of d or pre with an
- * argument are errors the library does not look for.  It runs on the kernel that quartet_mxfp4_gemm would take (quartet_debug_set_gemm_plan
- * included).  Fastest where n and all leading dimensions are multiples of 4.
+ * argument are errors the library does not look for.  It runs on the tiles that quartet_mxfp4_gemm would take (quartet_debug_set_gemm_plan
+ * included), with the same order of sums; results of 256 MiB and more are stored through the caches here.  Fastest where n and all leading
+ * dimensions are multiples of 4.
  */
 int quartet_mxfp4_gemm_act(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales,
                            int64_t m, int64_t n, int64_t k, float alpha, const void *bias, int bias_dtype, int activation,

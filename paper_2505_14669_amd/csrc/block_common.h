@@ -23,7 +23,8 @@ __device__ __forceinline__ uint4 pack8(const float* v) {
 }
 
 // Activations (QUARTET_ACT_*).  SiLU and GELU are z s(p(z)) with s(t) = 1 / (1 + exp(-t)); exp through the hardware's 2^x and the quotient through
-// its reciprocal, each good to about 1 ulp: the relative error stays near 2^-22 + |t| 2^-24, below every result's rounding but fp32's.
+// its reciprocal, each good to about 1 ulp: the relative error stays near 2^-22 + |t| 2^-24, below every result's rounding but fp32's.  A gate below 2^-126 (SiLU: z
+// below -87) may come out as 0: the reciprocal gives no subnormal numbers; the value is then off by less than 10^-35.
 enum Act { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282553447f;     // 2 c and 2 c 0.044715, c = sqrt(2 / pi)

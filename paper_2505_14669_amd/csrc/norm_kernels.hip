@@ -302,7 +302,9 @@ rmsnorm_fwd_kernel(NormFwdArgs a) {
 template <int WPR, int CH, bool PAST>
 __global__ void __launch_bounds__(WPR < 4 ? 256 : 64 * WPR)
 rmsnorm_bwd_kernel(NormBwdArgs a) {
-    constexpr bool AHEAD = WPR < 16 || CH == 1;      // (the wide rows' 1024 threads have no registers for two rows)
+    // Rows wider than 8192: 1024 threads leave 128 registers each, too few for the values of one row beside the sums: the compiler spills 84 bytes a lane up to
+    // 16384 columns and 676 beyond (us, and the bytes at 6.2 TB/s: 4096 x 11008 bf16 120 / 58, 4096 x 16384 145 / 87, 2048 x 32768 591 / 87; 4096 x 8192 54.6 / 43.3).
+    constexpr bool AHEAD = WPR < 16 || CH == 1;
     constexpr uint32_t THREADS = WPR < 4 ? 256 : 64 * WPR, RPB = THREADS / 64 / WPR;
     __shared__ float meet[2][THREADS / 64];
     __shared__ float4 join[RPB > 1 ? THREADS * 2 : 1];

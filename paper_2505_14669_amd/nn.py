@@ -123,7 +123,9 @@ _ANY = (torch.bfloat16, torch.float32)
 
 
 class _EpilogueFunction(torch.autograd.Function):
-    """a(x W^T + bias) * multiplier + residual: the layer's operands, its product with the epilogue, and both backward passes."""
+    """a(x W^T + bias) * multiplier + residual: the layer's operands, its product with the epilogue, and both backward passes.  The gradient of an fp32
+    result is rounded to bf16 before the gate, the slope, dmul and dbias (quartet_act_bwd and the layer's backward pass take bf16, and so does the gradient
+    that reaches a layer with a bf16 result); the residual's gradient stays as it came."""
 
     @staticmethod
     def forward(ctx, x, weight, bias, multiplier, residual, seed, rounding, hadamard_block, activation, graph):
@@ -208,9 +210,9 @@ class _EpilogueFunction(torch.autograd.Function):
 
 class QuartetLinear(torch.nn.Module):
     """nn.Linear replacement: weight [out, in] (bf16, or fp32 master weights cast to bf16 on the way
-    in), optional bf16 bias.  activation ("none", "relu", "gelu", "silu"), multiplier (bf16, the other branch of a gated layer) and
-    residual (bf16 or fp32, whose type the result then has) join the product's epilogue: a(x W^T + bias) * multiplier + residual; without
-    any of them the bias is added to the product's bf16 result.  Every backward pass uses a fresh stochastic-rounding seed: base seed, layer id and a
+    in), optional bf16 bias.  activation ("none", "relu", "gelu" in its tanh form: torch's approximate="tanh", "silu"), multiplier (bf16, the other branch
+    of a gated layer) and residual (bf16 or fp32, whose type the result then has) join the product's epilogue: a(x W^T + bias) * multiplier + residual; a
+    bias alone is added by torch to the product's bf16 result.  Every backward pass uses a fresh stochastic-rounding seed: base seed, layer id and a
     per-layer call counter packed into 64 bits, so runs are reproducible and no two calls share draws."""
     _next_id = 0
 
@@ -302,7 +304,8 @@ class _RMSNormFunction(torch.autograd.Function):
 
 class QuartetRMSNorm(torch.nn.Module):
     """y = h / sqrt(mean(h^2) + eps) * weight as bf16, what QuartetLinear takes.  forward(x): h = x.  forward(x, residual): h = residual + x in
-    residual's type, and the result is (y, h): the norm and the stream it leaves for the next layer.  x, residual [..., n] bf16 or fp32."""
+    residual's type, and the result is (y, h): the norm and the stream it leaves for the next layer.  x, residual [..., n] bf16 or fp32.  The backward pass
+    needs h as it is.  (block.quartet_rmsnorm_fwd also writes MXFP4 and MXFP8 operands; QuartetLinear makes its operand from y itself.)"""
 
     def __init__(self, n, eps=1e-5, device="cuda", weight_dtype=torch.float32):
         super().__init__()
