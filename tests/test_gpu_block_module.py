@@ -222,3 +222,57 @@ def test_layer_with_an_epilogue_over_no_tokens(nn, shape):
     assert lin.weight.grad.shape == (96, 64) and bool((lin.weight.grad == 0).all()) and lin.bias.grad.shape == (96,) and bool((lin.bias.grad == 0).all())
     with torch.no_grad():
         assert lin(x).shape == y.shape
+
+
+class GatedBlock(torch.nn.Module):
+    """norm, gated projections with bias and down projection onto the stream"""
+
+    def __init__(self, nn, d, h):
+        super().__init__()
+        self.norm, self.gate, self.up = nn.QuartetRMSNorm(d), nn.QuartetLinear(d, h, bias=True, activation="silu"), nn.QuartetLinear(d, h)
+        self.down = nn.QuartetLinear(h, d, bias=True)
+
+    def forward(self, x, stream):
+        for lin in (self.gate, self.up, self.down):
+            lin.calls = 0                                      # the same draws in every pass: a graph replays those of its capture
+        y, stream = self.norm(x, stream)
+        return self.down(self.gate(y, multiplier=self.up(y)), residual=stream)
+
+
+def test_block_captured_forward_and_backward(nn):
+    g = rng(10)
+    captured, eager = (GatedBlock(nn, 128, 256) for _ in range(2))
+    eager.load_state_dict(captured.state_dict())
+    for a, c in zip(captured.children(), eager.children()):
+        if a is not captured.norm:
+            c.layer_id = a.layer_id
+    inputs = [(new(g, 64, 128), new(g, 64, 128, dtype=F32), new(g, 64, 128, dtype=F32, scale=0.1)) for _ in range(3)]
+    x, stream, dy = (t.clone() for t in inputs[0])
+    x.requires_grad_()
+    stream.requires_grad_()
+    leaves = [x, stream, *captured.parameters()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured(x, stream).backward(dy)
+    torch.cuda.current_stream().wait_stream(side)
+    for t in leaves:
+        t.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = captured(x, stream)
+        out.backward(dy)
+        norm = nn.clip_grad_norm_(captured.parameters(), 0.01)
+    for turn in range(5):
+        with torch.no_grad():
+            for t, source in zip((x, stream, dy), inputs[turn % 3]):
+                t.copy_(source)
+        xe, se = (t.clone().requires_grad_() for t in inputs[turn % 3][:2])      # eager work between the replays, on leaves of its own
+        eager.zero_grad(set_to_none=True)
+        want = eager(xe, se)
+        want.backward(inputs[turn % 3][2])
+        want_norm = nn.clip_grad_norm_(eager.parameters(), 0.01)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(norm, want_norm) and float(norm) > 0.01, turn
+        assert all(torch.equal(a.grad, c.grad) for a, c in zip(leaves, [xe, se, *eager.parameters()])), turn
